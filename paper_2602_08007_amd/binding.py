@@ -22,9 +22,13 @@ __all__ = [
     "tsr_one_sided_workspace_bytes", "tsr_project_one_sided", "tsr_backproject_one_sided",
     "tsr_refresh_exact_workspace_bytes", "tsr_refresh_exact_svd",
     "tsr_matrix_desc", "tsr_hyper", "Plan", "workspace",
+    "TSR_E4M3", "TSR_E5M2", "TSR_STATE_F32", "TSR_STATE_8BIT", "TSR_STATE_BLOCK", "tsr_tensor_desc", "TensorSet",
+    "tsr_adamw_batched", "tsr_grad_norm_workspace_bytes", "tsr_grad_norm_batched",
+    "tsr_fp8_matrix", "fp8_matrix", "tsr_fp8_quantize", "tsr_fp8_matmul_workspace_bytes", "tsr_fp8_matmul",
 ]
 
-TSR_F32, TSR_BF16 = 0, 1
+TSR_F32, TSR_BF16, TSR_E4M3, TSR_E5M2 = 0, 1, 2, 3
+TSR_STATE_F32, TSR_STATE_8BIT, TSR_STATE_BLOCK = 0, 1, 256
 TSR_PREC_SPLIT, TSR_PREC_BF16 = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -53,6 +57,15 @@ class tsr_matrix_desc(ctypes.Structure):
 
 class tsr_hyper(ctypes.Structure):
     _fields_ = [("lr", _f), ("wd", _f), ("beta1", _f), ("beta2", _f), ("eps", _f), ("scale", _f)]
+
+
+class tsr_tensor_desc(ctypes.Structure):
+    _fields_ = [("p", _vp), ("g", _vp), ("m", _vp), ("v", _vp), ("m_scale", _vp), ("v_scale", _vp), ("p16", _vp),
+                ("count", _ll), ("p_dtype", _i), ("g_dtype", _i), ("state", _i), ("wd_scale", _f)]
+
+
+class tsr_fp8_matrix(ctypes.Structure):
+    _fields_ = [("q", _vp), ("scale", _vp), ("ld", _ll), ("ld_scale", _ll), ("dtype", _i), ("block_rows", _i)]
 
 
 def _sig(name, restype, *argtypes):
@@ -97,6 +110,15 @@ _refresh_batched = _sig("tsr_refresh_batched", _i, _vp, ctypes.POINTER(_vp), _i,
 _prof_begin = _sig("tsr_plan_profile_begin", _i, _vp)
 _prof_end = _sig("tsr_plan_profile_end", _i, _vp, _vp, ctypes.POINTER(_f), ctypes.POINTER(_i))
 _payload = _sig("tsr_plan_payload_bytes", None, _vp, _i, ctypes.POINTER(_ll), ctypes.POINTER(_ll))
+
+
+_adamw = _sig("tsr_adamw_batched", _i, ctypes.POINTER(tsr_tensor_desc), _i, _i, ctypes.POINTER(tsr_hyper), ctypes.c_ulonglong,
+              _vp, _vp)
+_norm_ws = _sig("tsr_grad_norm_workspace_bytes", _sz, ctypes.POINTER(tsr_tensor_desc), _i)
+_norm = _sig("tsr_grad_norm_batched", _i, ctypes.POINTER(tsr_tensor_desc), _i, _f, _vp, _vp, _vp, _sz, _vp)
+_quantize = _sig("tsr_fp8_quantize", _i, _vp, _i, _i, _i, _ll, _i, _i, _vp, _ll, _vp, _ll, _vp, _ll, _vp, _ll, _vp)
+_matmul_ws = _sig("tsr_fp8_matmul_workspace_bytes", _sz, _i, _i, _i)
+_matmul = _sig("tsr_fp8_matmul", _i, ctypes.POINTER(tsr_fp8_matrix), ctypes.POINTER(tsr_fp8_matrix), _i, _i, _i, _vp, _ll, _vp, _sz, _vp)
 
 
 class TsrError(RuntimeError):
@@ -414,3 +436,189 @@ class Plan:
             self.close()
         except Exception:
             pass
+
+
+# ------------------------------------------------------------------ parameters that are kept dense
+_FP8 = {torch.float8_e4m3fn: TSR_E4M3, torch.float8_e5m2: TSR_E5M2}
+
+
+def _device_of(*tensors) -> torch.device:
+    """The one GPU that all tensors (those that are not None) lie on."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError("tensors on different devices: %s and %s" % (dev, t.device))
+    if dev.type != "cuda":
+        raise TypeError("expected GPU tensors")
+    return dev
+
+
+def _launch(dev: torch.device, stream, fn, *args) -> None:
+    """fn(*args, stream) with the tensors' device current; the stream is that device's current one unless given."""
+    if isinstance(stream, torch.cuda.Stream) and stream.device != dev:
+        raise ValueError("the stream belongs to another device than the tensors")
+    if dev.index == torch.cuda.current_device():
+        _check(fn(*args, _stream(stream)))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, _stream(stream)))
+
+
+class TensorSet:
+    """The tensors of tsr_adamw_batched and tsr_grad_norm_batched, as the array the library takes.
+
+    tensors: sequence of dicts with p, g, m, v (m and v float32, or float8_e4m3fn and float8_e5m2 with m_scale, v_scale
+    uint8 of a value for each 256 elements), optionally p16 (bfloat16) and wd_scale (1 by default).  For the norm alone, g
+    is enough.  All contiguous, all on one device; the set keeps them alive and describes their storage as it is now."""
+
+    def __init__(self, tensors: Sequence[dict]):
+        self._keep = [dict(t) for t in tensors]
+        self.count = len(self._keep)
+        self.only_g = any("p" not in t for t in self._keep)
+        self.descs = (tsr_tensor_desc * max(self.count, 1))()
+        self.device = _device_of(*(x for t in self._keep for x in t.values() if isinstance(x, torch.Tensor)))
+        for d, t in zip(self.descs, self._keep):
+            g = t["g"]
+            for x in t.values():
+                if isinstance(x, torch.Tensor) and not x.is_contiguous():
+                    raise TypeError("expected contiguous tensors")
+            d.g, d.g_dtype, d.count = _ptr(g), _gdtype(g), g.numel()
+            d.wd_scale = t.get("wd_scale", 1.0)
+            if "p" not in t:
+                continue
+            p, m, v = t["p"], t["m"], t["v"]
+            if p.numel() != d.count or m.numel() != d.count or v.numel() != d.count:
+                raise ValueError("p, g, m and v must have as many elements")
+            d.p, d.p_dtype, d.m, d.v = _ptr(p), _gdtype(p), _ptr(m), _ptr(v)
+            if m.dtype == torch.float32 and v.dtype == torch.float32:
+                d.state = TSR_STATE_F32
+            elif m.dtype == torch.float8_e4m3fn and v.dtype == torch.float8_e5m2:
+                d.state = TSR_STATE_8BIT
+                blocks = -(-d.count // TSR_STATE_BLOCK)
+                for x in (t["m_scale"], t["v_scale"]):
+                    if x.dtype != torch.uint8 or x.numel() < blocks:
+                        raise ValueError("m_scale and v_scale must be uint8, a value for each %d elements" % TSR_STATE_BLOCK)
+                d.m_scale, d.v_scale = _ptr(t["m_scale"]), _ptr(t["v_scale"])
+            else:
+                raise TypeError("m and v must be float32, or float8_e4m3fn and float8_e5m2")
+            p16 = t.get("p16")
+            if p16 is not None:
+                if p16.dtype != torch.bfloat16 or p16.numel() != d.count:
+                    raise TypeError("p16 must be bfloat16 with as many elements as p")
+                d.p16 = _ptr(p16)
+
+
+def _tensor_set(tensors) -> TensorSet:
+    return tensors if isinstance(tensors, TensorSet) else TensorSet(tensors)
+
+
+def _scalar(t: Optional[torch.Tensor], name: str) -> None:
+    if t is not None and (t.dtype != torch.float32 or t.numel() != 1):
+        raise TypeError("%s must be one float32 value" % name)
+
+
+def tsr_adamw_batched(tensors, t, lr, wd=0.0, beta1=0.9, beta2=0.999, eps=1e-8, scale=1.0, g_scale=None, seed=0, stream=None):
+    """One AdamW step of all tensors (a TensorSet, or the dicts it is made of)."""
+    s = _tensor_set(tensors)
+    if s.only_g:
+        raise ValueError("every tensor needs p, g, m and v")
+    _scalar(g_scale, "g_scale")
+    if g_scale is not None and g_scale.device != s.device:
+        raise ValueError("g_scale must lie on the tensors' device")
+    h = tsr_hyper(lr, wd, beta1, beta2, eps, scale)
+    _launch(s.device, stream, _adamw, s.descs, s.count, t, ctypes.byref(h), seed, _ptr(g_scale))
+
+
+def tsr_grad_norm_workspace_bytes(tensors) -> int:
+    s = _tensor_set(tensors)
+    return int(_norm_ws(s.descs, s.count))
+
+
+def tsr_grad_norm_batched(tensors, max_norm, norm, coef=None, ws=None, stream=None):
+    """norm (one float32 value) <- the norm of all g; coef <- what brings it to max_norm at most."""
+    s = _tensor_set(tensors)
+    _scalar(norm, "norm")
+    _scalar(coef, "coef")
+    dev = _device_of(norm, coef, ws)
+    if dev != s.device:
+        raise ValueError("norm, coef and ws must lie on the tensors' device")
+    if ws is None:
+        ws = _temp_workspace(tsr_grad_norm_workspace_bytes(s), dev, stream)
+    _launch(dev, stream, _norm, s.descs, s.count, max_norm, _ptr(norm), _ptr(coef), _ptr(ws), ws.numel())
+    return norm
+
+
+# ------------------------------------------------------------------ 8-bit matrices
+def fp8_matrix(rows: int, cols: int, dtype=torch.float8_e4m3fn, block_rows=1, device="cuda"):
+    """Place for an 8-bit matrix as the calls below take it: (q, scale), q rows x cols of a float8 type with rows padded to 16
+    bytes, scale uint8 ceil(rows / block_rows) x ceil(cols / 128) with rows padded to 4."""
+    q = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.uint8, device=device).view(dtype)[:, :cols]
+    s = torch.empty(-(-rows // block_rows), -(-cols // 512) * 4, dtype=torch.uint8, device=device)[:, :-(-cols // 128)]
+    return q, s
+
+
+def _fp8(q: torch.Tensor) -> int:
+    if q.dtype not in _FP8:
+        raise TypeError("expected float8_e4m3fn or float8_e5m2")
+    return _FP8[q.dtype]
+
+
+def _fp8_place(q, s, rows, cols, block_rows, name):
+    """(pointer, ld, scale pointer, ld) of an output of the quantiser, or four empty places."""
+    if q is None:
+        return None, 0, None, 0
+    if tuple(q.shape) != (rows, cols) or s.dtype != torch.uint8 or tuple(s.shape) != (-(-rows // block_rows), -(-cols // 128)):
+        raise ValueError("%s must be %d x %d with a uint8 scale for each %d x 128 of it" % (name, rows, cols, block_rows))
+    return _ptr(q), _rows_ld(q), _ptr(s), _rows_ld(s)
+
+
+def _rows_ld(t: torch.Tensor) -> int:
+    """Leading dimension; that of a single column or row may be anything in torch, and is made one that holds the row."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise TypeError("expected a row-major 2-D tensor (unit column stride)")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), -(-t.shape[1] // 16) * 16)
+
+
+def tsr_fp8_quantize(X, Q=None, S=None, Qt=None, St=None, block_rows=1, stream=None):
+    """X (float32 or bfloat16) into Q with scales S, and / or transposed into Qt with St (fp8_matrix makes such pairs)."""
+    m, n = X.shape
+    dev = _device_of(X, Q, S, Qt, St)
+    some = Q if Q is not None else Qt
+    if some is None or (Q is not None and Qt is not None and Q.dtype != Qt.dtype):
+        raise ValueError("give Q, Qt or both, of one type")
+    q, ldq, s, lds = _fp8_place(Q, S, m, n, block_rows, "Q")
+    qt, ldqt, st, ldst = _fp8_place(Qt, St, n, m, block_rows, "Qt")
+    _launch(dev, stream, _quantize, _ptr(X), _gdtype(X), m, n, _ld(X), block_rows, _fp8(some), q, ldq, s, lds, qt, ldqt, st, ldst)
+
+
+def _fp8_operand(q, s, k, name) -> tsr_fp8_matrix:
+    rows = q.shape[0]
+    if s.dtype != torch.uint8 or s.dim() != 2 or s.shape[1] != -(-k // 128) or s.shape[0] not in (rows, -(-rows // 128)):
+        raise ValueError("the scales of %s must be uint8, one for each 128 values of a row or of 128 rows" % name)
+    return tsr_fp8_matrix(_ptr(q), _ptr(s), _rows_ld(q), _rows_ld(s), _fp8(q), 1 if s.shape[0] == rows else 128)
+
+
+def tsr_fp8_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(_matmul_ws(m, n, k))
+
+
+def tsr_fp8_matmul(A, SA, B, SB, C, ws=None, stream=None):
+    """C (m x n, bfloat16) <- A B^T, A (m x k) and B (n x k) 8-bit with scales SA and SB."""
+    m, k = A.shape
+    n = B.shape[0]
+    dev = _device_of(A, SA, B, SB, C, ws)
+    if B.shape[1] != k or tuple(C.shape) != (m, n):
+        raise ValueError("A m x k, B n x k and C m x n do not fit")
+    if C.dtype != torch.bfloat16:
+        raise TypeError("C must be bfloat16")
+    if ws is None:
+        nbytes = tsr_fp8_matmul_workspace_bytes(m, n, k)
+        ws = _temp_workspace(nbytes, dev, stream) if nbytes else None
+    a, b = _fp8_operand(A, SA, k, "A"), _fp8_operand(B, SB, k, "B")
+    _launch(dev, stream, _matmul, ctypes.byref(a), ctypes.byref(b), m, n, k, _ptr(C), _rows_ld(C), _ptr(ws),
+            0 if ws is None else ws.numel())
+    return C

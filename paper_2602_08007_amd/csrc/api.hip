@@ -921,6 +921,7 @@ const char* tsr_status_string(int status) {
         case TSR_BAD_DTYPE: return "bad dtype";
         case TSR_WORKSPACE_TOO_SMALL: return "workspace too small";
         case TSR_HIP_ERROR: return "HIP runtime error";
+        case TSR_OUT_OF_HOST_MEMORY: return "out of host memory";
         case TSR_STATIC_SCRATCH_TOO_SMALL: return "problem needs more scratch than the built-in static buffer holds";
         default: return "unknown status";
     }
@@ -1038,15 +1039,6 @@ int tsr_stream_scale(float* dst, const float* src, long long count, float scale,
 }
 
 // ---------------------------------------------------------------- Adam / SGD on the core
-static int adam_scalars(AdamScalars& s, int t, float beta1, float beta2, float eps) {
-    if (t < 1) return TSR_INVALID_ARG;
-    if (!(beta1 >= 0.0f && beta1 < 1.0f) || !(beta2 >= 0.0f && beta2 < 1.0f) || !(eps >= 0.0f)) return TSR_INVALID_ARG;
-    s.beta1 = beta1; s.beta2 = beta2; s.eps = eps;
-    s.inv_c1 = (float)(1.0 / (1.0 - std::pow((double)beta1, (double)t)));
-    s.inv_c2 = (float)(1.0 / (1.0 - std::pow((double)beta2, (double)t)));
-    return TSR_OK;
-}
-
 int tsr_adam_core(const float* C, float* M, float* Vm, float* D, long long count, int t, float beta1, float beta2,
                   float eps, void* stream) {
     if (!C || !M || !Vm || !D) return TSR_INVALID_ARG;

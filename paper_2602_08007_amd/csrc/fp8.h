@@ -1,0 +1,28 @@
+// 8-bit matrices with a scale for each block of 128: how they are made and multiplied (internal interface).
+#pragma once
+#include <hip/hip_runtime.h>
+
+namespace tsr {
+
+struct QuantizeArgs {
+    const void* X; long long ldx; int x_bf16;
+    int m, n;
+    unsigned char* Q; long long ldq; unsigned char* S; long long lds;            // as stored, or null
+    unsigned char* Qt; long long ldqt; unsigned char* St; long long ldst;        // transposed, or null
+};
+hipError_t launch_fp8_quantize(const QuantizeArgs& a, int fmt, int block_rows, hipStream_t stream);
+
+// One operand: rows x k bytes, and a scale byte for each 128 of them and 1 << shift rows.
+struct Fp8Operand {
+    const unsigned char* q; const unsigned char* scale;
+    long long ld, ld_scale;
+    int rows, shift;
+};
+struct Fp8Args {
+    Fp8Operand a, b;            // C is a.rows x b.rows
+    int k;
+    void* C; long long ldc;     // bf16
+};
+hipError_t launch_fp8_matmul(const Fp8Args& a, int fmt_a, int fmt_b, hipStream_t stream);
+
+}  // namespace tsr

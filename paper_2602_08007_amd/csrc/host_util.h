@@ -2,11 +2,13 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdint>
 #include <cstring>
 #include <vector>
 
 #include "../../include/tsr.h"
+#include "small.h"
 
 namespace tsr {
 
@@ -47,6 +49,15 @@ struct Arena {
 };
 
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+inline int adam_scalars(AdamScalars& s, int t, float beta1, float beta2, float eps) {
+    if (t < 1) return TSR_INVALID_ARG;
+    if (!(beta1 >= 0.0f && beta1 < 1.0f) || !(beta2 >= 0.0f && beta2 < 1.0f) || !(eps >= 0.0f)) return TSR_INVALID_ARG;
+    s.beta1 = beta1; s.beta2 = beta2; s.eps = eps;
+    s.inv_c1 = (float)(1.0 / (1.0 - std::pow((double)beta1, (double)t)));
+    s.inv_c2 = (float)(1.0 / (1.0 - std::pow((double)beta2, (double)t)));
+    return TSR_OK;
+}
 
 // Optional per-stage timing: HIP events recorded on the work stream around every stage.
 struct Prof {

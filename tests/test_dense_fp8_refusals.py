@@ -1,0 +1,142 @@
+"""What the calls on dense parameters and 8-bit matrices refuse, on the host, before anything is launched."""
+import ctypes
+
+import pytest
+
+FAKE = 0x10000          # never dereferenced: every call below fails its checks first
+OK = 0
+
+
+@pytest.fixture(scope="module")
+def tsr():
+    import paper_2602_08007_amd as t
+    return t
+
+
+def tensors(tsr, number=1, **change):
+    d = (tsr.tsr_tensor_desc * number)()
+    for i in range(number):
+        at = FAKE + i * 0x100000
+        d[i].p, d[i].g, d[i].m, d[i].v = at, at + 0x10000, at + 0x20000, at + 0x30000
+        d[i].count, d[i].wd_scale = 100, 1.0
+    for k, v in change.items():
+        setattr(d[number - 1], k, v)
+    return d
+
+
+def adamw(tsr, d, count=None, t=1, beta1=0.9, beta2=0.999, eps=1e-8, hyper=True, g_scale=None):
+    h = tsr.tsr_hyper(1e-3, 0.1, beta1, beta2, eps, 1.0)
+    return tsr.lib.tsr_adamw_batched(d, len(d) if count is None and d is not None else count or 0, t, ctypes.byref(h) if hyper else None, 0, g_scale, None)
+
+
+def test_sizes_of_the_descriptions(tsr):
+    assert ctypes.sizeof(tsr.tsr_tensor_desc) == 80 and ctypes.sizeof(tsr.tsr_fp8_matrix) == 40
+    assert "memory" in tsr.tsr_status_string(-7)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(p=None), -1), (dict(g=None), -1), (dict(m=None), -1), (dict(v=None), -1),
+    (dict(p=FAKE + 2), -1), (dict(g=FAKE + 0x10002), -1), (dict(m=FAKE + 0x20001), -1), (dict(v=FAKE + 0x30002), -1),
+    (dict(p_dtype=1, p=FAKE + 1), -1), (dict(g_dtype=1, g=FAKE + 0x10001), -1),
+    (dict(p_dtype=2), -3), (dict(g_dtype=3), -3), (dict(p_dtype=-1), -3), (dict(state=2), -3),
+    (dict(count=-1), -2), (dict(count=(1 << 35) + 1), -2),
+    (dict(state=1), -1), (dict(state=1, m_scale=FAKE + 0x40000), -1),
+    (dict(p16=FAKE + 0x50001), -1), (dict(p16=FAKE + 0x50000, p_dtype=1), -1),
+    (dict(wd_scale=float("nan")), -1), (dict(wd_scale=float("inf")), -1),
+    # ranges that are written and meet: within a tensor, by one element, with a state's scales, with the bf16 copy
+    (dict(m=FAKE), -1), (dict(v=FAKE + 0x20000 + 396), -1), (dict(p16=FAKE + 398), -1),
+    (dict(state=1, m_scale=FAKE + 0x40000, v_scale=FAKE + 0x40000), -1), (dict(state=1, m_scale=FAKE + 0x20000 + 99, v_scale=FAKE + 0x40000), -1)])
+def test_a_tensor_that_does_not_fit(tsr, change, status):
+    assert adamw(tsr, tensors(tsr, **change)) == status
+
+
+def test_tensors_that_meet_each_other(tsr):
+    for change in (dict(p=FAKE), dict(p=FAKE + 396), dict(m=FAKE + 0x30000), dict(p16=FAKE + 4)):
+        assert adamw(tsr, tensors(tsr, 2, **change)) == -1
+    many = tensors(tsr, 200, v=FAKE + 55 * 0x100000)
+    assert adamw(tsr, many) == -1
+
+
+def test_the_arguments_of_a_step(tsr):
+    d = tensors(tsr)
+    assert adamw(tsr, None, 1) == -1
+    assert adamw(tsr, d, hyper=False) == -1
+    assert tsr.lib.tsr_adamw_batched(d, 0, 1, ctypes.byref(tsr.tsr_hyper()), 0, None, None) == -2
+    assert tsr.lib.tsr_adamw_batched(d, -3, 1, ctypes.byref(tsr.tsr_hyper()), 0, None, None) == -2
+    assert adamw(tsr, d, t=0) == -1
+    assert adamw(tsr, d, beta1=1.0) == -1 and adamw(tsr, d, beta2=-0.1) == -1 and adamw(tsr, d, eps=float("nan")) == -1
+    assert adamw(tsr, d, g_scale=FAKE + 1) == -1
+
+
+def test_a_step_of_nothing_launches_nothing(tsr):
+    d = (tsr.tsr_tensor_desc * 3)()                      # counts of zero: no pointer is needed
+    assert adamw(tsr, d) == OK
+
+
+def test_norm(tsr):
+    f, d = tsr.lib.tsr_grad_norm_batched, tensors(tsr, 3)
+    nbytes = tsr.lib.tsr_grad_norm_workspace_bytes(d, 3)
+    assert nbytes >= 3 * 8 and nbytes % 256 == 0
+    assert f(None, 3, 1.0, FAKE, None, FAKE, nbytes, None) == -1
+    assert f(d, 0, 1.0, FAKE, None, FAKE, nbytes, None) == -2
+    assert f(d, 3, 0.0, FAKE, None, FAKE, nbytes, None) == -1 and f(d, 3, float("nan"), FAKE, None, FAKE, nbytes, None) == -1
+    assert f(d, 3, 1.0, None, None, FAKE, nbytes, None) == -1 and f(d, 3, 1.0, FAKE + 2, None, FAKE, nbytes, None) == -1
+    assert f(d, 3, 1.0, FAKE, FAKE, FAKE, nbytes, None) == -1                    # norm and coef are two places
+    assert f(d, 3, 1.0, FAKE, None, None, nbytes, None) == -1 and f(d, 3, 1.0, FAKE, None, FAKE + 8, nbytes, None) == -1
+    assert f(d, 3, 1.0, FAKE, None, FAKE, 16, None) == -4
+    for change, status in ((dict(count=-1), -2), (dict(g=None), -1), (dict(g_dtype=2), -3), (dict(g=FAKE + 2), -1)):
+        bad = tensors(tsr, 3, **change)
+        assert f(bad, 3, 1.0, FAKE, None, FAKE, 1 << 20, None) == status
+        assert tsr.lib.tsr_grad_norm_workspace_bytes(bad, 3) == 0
+    assert tsr.lib.tsr_grad_norm_workspace_bytes(None, 3) == 0 and tsr.lib.tsr_grad_norm_workspace_bytes(d, 0) == 0
+    # the number of partial sums is bounded, whatever the tensors hold
+    big = tensors(tsr, 300)
+    for x in big:
+        x.count = 1 << 35
+    assert 0 < tsr.lib.tsr_grad_norm_workspace_bytes(big, 300) <= (4096 + 300) * 8 + 256
+
+
+def test_quantize(tsr):
+    def call(X=FAKE, xt=0, m=10, n=200, ldx=200, rows=1, qt=2, Q=FAKE, ldq=208, S=FAKE, lds=4, T=FAKE, ldt=16, St=FAKE, ldst=4):
+        return tsr.lib.tsr_fp8_quantize(X, xt, m, n, ldx, rows, qt, Q, ldq, S, lds, T, ldt, St, ldst, None)
+    for change, status in (
+            (dict(X=None), -1), (dict(X=FAKE + 2), -1), (dict(X=FAKE + 1, xt=1), -1), (dict(xt=2), -3), (dict(qt=0), -3), (dict(qt=4), -3),
+            (dict(m=0), -2), (dict(n=-1), -2), (dict(ldx=199), -2), (dict(rows=64), -2), (dict(rows=0), -2),
+            (dict(Q=None, T=None), -1), (dict(Q=FAKE + 8), -1), (dict(ldq=200), -1), (dict(ldq=192), -2), (dict(S=None), -1), (dict(S=FAKE + 2), -1),
+            (dict(lds=2), -1), (dict(lds=1), -2), (dict(T=FAKE + 1), -1), (dict(ldt=10), -1), (dict(ldt=8), -2), (dict(St=None), -1), (dict(ldst=3), -1),
+            (dict(ldst=0), -2)):
+        assert call(**change) == status, change
+
+
+def test_matmul(tsr):
+    def operand(**change):
+        x = tsr.tsr_fp8_matrix(FAKE, FAKE, 208, 4, 2, 1)
+        for k, v in change.items():
+            setattr(x, k, v)
+        return x
+    def call(a=None, b=None, m=10, n=20, k=200, C=FAKE, ldc=20, ws=FAKE, nbytes=1 << 40):
+        a, b = operand() if a is None else a, operand() if b is None else b
+        return tsr.lib.tsr_fp8_matmul(ctypes.byref(a), ctypes.byref(b), m, n, k, C, ldc, ws, nbytes, None)
+    for change, status in ((dict(m=0), -2), (dict(n=0), -2), (dict(k=0), -2), (dict(k=(1 << 22) + 1), -2), (dict(ldc=19), -2), (dict(C=None), -1), (dict(C=FAKE + 1), -1)):
+        assert call(**change) == status, change
+    for change, status in ((dict(q=None), -1), (dict(scale=None), -1), (dict(q=FAKE + 8), -1), (dict(ld=200), -1), (dict(ld=192), -2), (dict(scale=FAKE + 1), -1),
+                           (dict(ld_scale=1), -2), (dict(ld_scale=2), -1), (dict(dtype=1), -3), (dict(dtype=4), -3), (dict(block_rows=2), -2)):
+        assert call(a=operand(**change)) == status, change
+        assert call(b=operand(**change)) == status, change
+    assert tsr.lib.tsr_fp8_matmul(None, ctypes.byref(operand()), 10, 20, 200, FAKE, 20, None, 0, None) == -1
+    assert tsr.tsr_fp8_matmul_workspace_bytes(0, 1, 1) == 0
+
+
+def test_other_calls_know_nothing_of_8_bit_types(tsr):
+    f = tsr.lib.tsr_project_core
+    assert f(ctypes.c_void_p(FAKE), 2, 8, 8, ctypes.c_longlong(8), ctypes.c_void_p(FAKE), ctypes.c_void_p(FAKE), 4, ctypes.c_float(1.0), 0, ctypes.c_void_p(FAKE), 0,
+             ctypes.c_void_p(FAKE), ctypes.c_size_t(1 << 30), None) == -3
+
+
+def test_tensors_on_the_cpu_are_refused(tsr):
+    import torch
+    x = torch.zeros(8)
+    with pytest.raises(TypeError):
+        tsr.TensorSet([dict(p=x, g=x, m=x, v=x)])
+    with pytest.raises(TypeError):
+        tsr.tsr_fp8_quantize(torch.zeros(4, 4), *tsr.fp8_matrix(4, 4, device="cpu"))
