@@ -1,5 +1,8 @@
 // 8-bit floating point with a power of two as the scale of each block of 128: the quantiser, and C = A B^T on the scaled
 // matrix instructions of gfx950.
+#include <type_traits>
+
+#include "device_lds.h"
 #include "fp8.h"
 #include "fp8_format.h"
 
@@ -258,7 +261,235 @@ __global__ __launch_bounds__(256) void fp8_direct_kernel(const Fp8Args g) {
     }
 }
 
+// ------------------------------------------------------------------ product, tiles through LDS
+// A workgroup of four waves (2 x 2) computes 64 FM x 64 FN elements of C, each wave FM x FN tiles of 32 x 32, in steps of 64
+// along the contraction.  Rows of A and B go from memory straight into LDS (no registers between), four steps deep: what step t
+// overwrites was read in step t - 1, and is needed in step t + 3.  The fragments of step t + 1 are read while step t multiplies.
+// LDS rows are 64 bytes, four chunks of 16; chunk c of row r sits at c ^ ((r >> 1) & 3), which keeps the fragment reads free of
+// bank conflicts.  The 32 rows of B of a tile are kept in the order in which the instruction hands its results out, so that a
+// lane ends up with 16 neighbouring elements of a row of C: row 8 j + 4 h + i of the instruction is row 16 h + 4 j + i of B.
+// Scale bytes go through LDS too: for every block of 128 (two steps) the word that holds its byte, again for each of its four
+// blocks, so that a pair of steps is free of branches: the compiler moves matrix instructions across those.
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+__device__ inline i32x4 lds_rsrc(const void* p, long long bytes) {
+    const unsigned long long a = (unsigned long long)p;
+    return i32x4{(int)(unsigned)a, (int)((unsigned)(a >> 32) & 0xffffu), (int)(bytes > 0x7fffffffLL ? 0x7fffffffLL : bytes), 0x00020000};
+}
+// 16 (or 4) bytes a lane from `rsrc` + voff to LDS at `to` + 16 (or 4) times the lane.  Not known to the compiler's counting
+// of loads in flight: whoever reads the place waits by wait_loads and a barrier.  m0 is set where it is used, and nothing else in
+// this file lives there; it is read one wait state later (s_nop).
+__device__ inline void load_lds16(i32x4 rsrc, unsigned voff, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "memory");
+}
+__device__ inline void load_lds4(i32x4 rsrc, unsigned voff, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "memory");
+}
+template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+#define TSR_PIN __builtin_amdgcn_sched_barrier(0)
+
+template <int FM, int FN> struct TileLds {
+    static constexpr int ROWS = 64 * (FM + FN), BUF = ROWS * 64, DEPTH = 4;
+    static constexpr int SCALES = DEPTH * BUF, BYTES = SCALES + 4 * ROWS * 4;
+};
+
+template <int FA, int FB, int FM, int FN>
+__global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void fp8_tile_kernel(const Fp8Args g) {
+    using L = TileLds<FM, FN>;
+    constexpr int TM = 64 * FM, TN = 64 * FN, NF = FM + FN, NM = FM * FN;
+    constexpr unsigned OUT = 0x80000000u;                    // an offset beyond every operand: no access
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, h = lane >> 5, wm = wave >> 1, wn = wave & 1;
+
+    // The tile.  Workgroups go round the 8 XCDs; each XCD takes a run of neighbouring tiles, in bands of 8 rows of tiles, so that
+    // the tiles at work together share rows of A and B in its L2.
+    const int tiles_m = (g.a.rows + TM - 1) / TM, tiles_n = (g.b.rows + TN - 1) / TN, tiles = tiles_m * tiles_n;
+    const int xcd = blockIdx.x & 7, per = tiles >> 3, more = tiles & 7;
+    const int at = xcd * per + min(xcd, more) + (int)(blockIdx.x >> 3);
+    const int band = at / (8 * tiles_n), in_band = at - band * 8 * tiles_n, band_rows = min(8, tiles_m - band * 8);
+    const int m0 = (band * 8 + in_band % band_rows) * TM, n0 = in_band / band_rows * TN;
+
+    const int k16 = (g.k + 15) & ~15, nk = (g.k + 63) >> 6;
+    const int ma = min(TM, g.a.rows - m0) - 1, nb = min(TN, g.b.rows - n0) - 1;      // last row of each operand's tile
+    const i32x4 ra = lds_rsrc(g.a.q + m0 * g.a.ld, ma * g.a.ld + k16);
+    const i32x4 rb = lds_rsrc(g.b.q + n0 * g.b.ld, nb * g.b.ld + k16);
+    const int sk = ((g.k + 511) >> 9) * 4;                   // scale bytes of a row in whole words, which the row's pitch holds
+    const int sa0 = m0 >> g.a.shift, sb0 = n0 >> g.b.shift;
+    const i32x4 rsa = lds_rsrc(g.a.scale + sa0 * g.a.ld_scale, (((m0 + ma) >> g.a.shift) - sa0) * g.a.ld_scale + sk);
+    const i32x4 rsb = lds_rsrc(g.b.scale + sb0 * g.b.ld_scale, (((n0 + nb) >> g.b.shift) - sb0) * g.b.ld_scale + sk);
+
+    // Loads of a step: wave w brings rows 16 FM w .. of A and 16 FN w .. of B, 16 rows an instruction.  Rows beyond the operand
+    // repeat its last one; nothing of them is stored.
+    auto n_of = [](int r) { return (r & ~31) + ((r & 4) << 2) + ((r >> 3) & 3) * 4 + (r & 3); };
+    unsigned off[NF];
+#pragma unroll
+    for (int x = 0; x < NF; ++x) {
+        const int r = (x < FM ? wave * 16 * FM + x * 16 : wave * 16 * FN + (x - FM) * 16) + (lane >> 2);
+        const int c = ((lane & 3) ^ ((r >> 1) & 3)) * 16;
+        off[x] = (x < FM ? (unsigned)(min(r, ma) * g.a.ld) : (unsigned)(min(n_of(r), nb) * g.b.ld)) + c;
+    }
+    const unsigned base = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char*)lds;
+    auto load_one = [&](int t, int x) {                      // part x of step t into its buffer
+        const unsigned to = base + (t & 3) * L::BUF + (x < FM ? wave * 16 * FM + x * 16 : TM + wave * 16 * FN + (x - FM) * 16) * 64;
+        const unsigned v = t < nk ? off[x] + (unsigned)t * 64 : OUT;
+        load_lds16(x < FM ? ra : rb, v, to);
+    };
+    // Scales of block p: a word for each row of the tile's A rows, then of its B rows; wave w brings 64 SL of them.
+    constexpr int SL = (L::ROWS + 255) / 256;
+    static_assert(L::ROWS % 256 == 0 && TM % 64 == 0, "all lanes of an instruction on one side");
+    unsigned soff[SL];
+#pragma unroll
+    for (int x = 0; x < SL; ++x) {
+        const int r = (wave * SL + x) * 64 + lane;
+        soff[x] = r < TM ? (unsigned)((((m0 + min(r, ma)) >> g.a.shift) - sa0) * g.a.ld_scale)
+                         : (unsigned)((((n0 + min(n_of(r - TM), nb)) >> g.b.shift) - sb0) * g.b.ld_scale);
+    }
+    const int np = (g.k + 127) >> 7;
+    auto load_scales = [&](int p) {
+#pragma unroll
+        for (int x = 0; x < SL; ++x) {
+            const int r = (wave * SL + x) * 64;
+            const unsigned to = base + L::SCALES + ((p & 3) * L::ROWS + r) * 4;
+            load_lds4(r < TM ? rsa : rsb, p < np ? soff[x] + (p & ~3) : OUT, to);
+        }
+    };
+
+    f32x16 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    i32x8 F[2][NF];
+    unsigned sn[NF];
+    int s[NF];
+    // where this lane's two chunks of fragment f lie in a buffer
+    const int key = (l32 >> 1) & 3;
+    const int fa = (wm * FM * 32 + l32) * 64, fb = (TM + wn * FN * 32 + l32) * 64;
+    const int c0 = ((2 * h) ^ key) * 16, c1 = ((2 * h + 1) ^ key) * 16;
+    auto read = [&](int slot, int t, int f) {
+        const unsigned char* from = lds + (t & 3) * L::BUF + (f < FM ? fa + f * 2048 : fb + (f - FM) * 2048);
+        F[slot][f] = __builtin_shufflevector(*(const i32x4*)(from + c0), *(const i32x4*)(from + c1), 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    auto read_scale = [&](int p, int f) {
+        const int r = f < FM ? wm * FM * 32 + f * 32 + l32 : TM + wn * FN * 32 + (f - FM) * 32 + l32;
+        sn[f] = *(const unsigned*)(lds + L::SCALES + ((p & 3) * L::ROWS + r) * 4);
+    };
+
+    load_scales(0);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        if (t == 2) load_scales(1);
+#pragma unroll
+        for (int x = 0; x < NF; ++x) load_one(t, x);
+    }
+    wait_loads<3 * NF + SL>();                               // step 0 and its scales
+    __builtin_amdgcn_s_barrier();
+    TSR_PIN;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) read(0, 0, f);
+#pragma unroll
+    for (int f = 0; f < NF; ++f) read_scale(0, f);
+
+    // Step t (= slot, modulo 2) of block p.  TAIL: what lies beyond k is not part of the sum.
+    auto step = [&](int slot, int p, auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        const int t = 2 * p + slot;
+        // the loads of step t + 1 have landed, everybody's, and everybody has the fragments of step t: in flight may be
+        // what steps t - 1 and t - 2 began
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wait_loads<2 * NF + SL>();
+        __builtin_amdgcn_s_barrier();
+        TSR_PIN;
+        if (slot == 0) {
+#pragma unroll
+            for (int f = 0; f < NF; ++f) s[f] = (int)(sn[f] >> ((p & 3) * 8));
+            load_scales(p + 2);
+        }
+        if constexpr (TAIL) {
+#pragma unroll
+            for (int f = 0; f < NF; ++f) F[slot][f] = keep_bytes(F[slot][f], g.k - t * 64 - h * 32);
+        }
+        TSR_PIN;
+#pragma unroll
+        for (int q = 0; q < NM; ++q) {
+            const int i = q / FN, j = q % FN;
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(F[slot][FM + j], F[slot][i], acc[i][j], FB, FA, 0, s[FM + j], 0, s[i]);
+            TSR_PIN;
+            // the fragments of the next step (and the scales of the next block) beside the first half, loads beside the second
+            constexpr int HALF = NM / 2;
+            if (q < HALF) {
+#pragma unroll
+                for (int f = q * NF / HALF; f < (q + 1) * NF / HALF; ++f) {
+                    read(slot ^ 1, t + 1, f);
+                    if (slot == 1) read_scale(p + 1, f);
+                }
+            } else {
+#pragma unroll
+                for (int x = (q - HALF) * NF / HALF; x < (q - HALF + 1) * NF / HALF; ++x) load_one(t + 4, x);
+            }
+            TSR_PIN;
+        }
+    };
+    const int whole = g.k >> 7;
+    for (int p = 0; p < whole; ++p) {
+        step(0, p, std::false_type{});
+        step(1, p, std::false_type{});
+    }
+    if (g.k & 127) {
+        step(0, whole, std::true_type{});
+        step(1, whole, std::true_type{});
+    }
+    wait_loads<0>();                                         // nothing may land after this workgroup's LDS is another's
+
+    const bool vec = ((unsigned long long)g.C & 15) == 0 && (g.ldc & 7) == 0;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int m = m0 + wm * FM * 32 + i * 32 + l32;
+        if (m >= g.a.rows) continue;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int n = n0 + wn * FN * 32 + j * 32 + h * 16;
+            __bf16* to = (__bf16*)g.C + (long long)m * g.ldc + n;
+            typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+            if (vec && n + 16 <= g.b.rows) {
+                bf16x8 lo, hi;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { lo[e] = (__bf16)acc[i][j][e]; hi[e] = (__bf16)acc[i][j][8 + e]; }
+                *(bf16x8*)to = lo;
+                *(bf16x8*)(to + 8) = hi;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) if (n + e < g.b.rows) to[e] = (__bf16)acc[i][j][e];
+            }
+        }
+    }
+}
+
+template <int FA, int FB> hipError_t launch_tiles(const Fp8Args& a, int shape, hipStream_t stream) {
+    const int t = shape == 0 ? 256 : 128;
+    const long long tiles = (long long)((a.a.rows + t - 1) / t) * ((a.b.rows + t - 1) / t);
+    const int bytes = shape == 0 ? TileLds<4, 4>::BYTES : TileLds<2, 2>::BYTES;
+    const void* k = shape == 0 ? (const void*)fp8_tile_kernel<FA, FB, 4, 4> : (const void*)fp8_tile_kernel<FA, FB, 2, 2>;
+    const hipError_t e = allow_lds(k, bytes);
+    if (e != hipSuccess) return e;
+    if (shape == 0) hipLaunchKernelGGL((fp8_tile_kernel<FA, FB, 4, 4>), dim3((unsigned)tiles), dim3(256), bytes, stream, a);
+    else hipLaunchKernelGGL((fp8_tile_kernel<FA, FB, 2, 2>), dim3((unsigned)tiles), dim3(256), bytes, stream, a);
+    return hipGetLastError();
+}
+
 hipError_t launch_fp8_matmul(const Fp8Args& a, int fmt_a, int fmt_b, hipStream_t stream) {
+    if (a.a.rows > 64 && a.b.rows > 64) {
+        const long long wide = (long long)((a.a.rows + 255) / 256) * ((a.b.rows + 255) / 256);
+        const int shape = wide >= 256 ? 0 : 1;
+        if (fmt_a == FP8_E4M3 && fmt_b == FP8_E4M3) return launch_tiles<0, 0>(a, shape, stream);
+        if (fmt_a == FP8_E4M3) return launch_tiles<0, 1>(a, shape, stream);
+        if (fmt_b == FP8_E4M3) return launch_tiles<1, 0>(a, shape, stream);
+        return launch_tiles<1, 1>(a, shape, stream);
+    }
     const dim3 grid((unsigned)((a.b.rows + 15) / 16), (unsigned)((a.a.rows + 63) / 64));
     if (fmt_a == FP8_E4M3 && fmt_b == FP8_E4M3) hipLaunchKernelGGL((fp8_direct_kernel<0, 0, 4>), grid, dim3(256), 0, stream, a);
     else if (fmt_a == FP8_E4M3) hipLaunchKernelGGL((fp8_direct_kernel<0, 1, 4>), grid, dim3(256), 0, stream, a);
