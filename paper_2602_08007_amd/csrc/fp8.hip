@@ -262,14 +262,17 @@ __global__ __launch_bounds__(256) void fp8_direct_kernel(const Fp8Args g) {
 }
 
 // ------------------------------------------------------------------ product, tiles through LDS
-// A workgroup of four waves (2 x 2) computes 64 FM x 64 FN elements of C, each wave FM x FN tiles of 32 x 32, in steps of 64
-// along the contraction.  Rows of A and B go from memory straight into LDS (no registers between), four steps deep: what step t
-// overwrites was read in step t - 1, and is needed in step t + 3.  The fragments of step t + 1 are read while step t multiplies.
-// LDS rows are 64 bytes, four chunks of 16; chunk c of row r sits at c ^ ((r >> 1) & 3), which keeps the fragment reads free of
-// bank conflicts.  The 32 rows of B of a tile are kept in the order in which the instruction hands its results out, so that a
-// lane ends up with 16 neighbouring elements of a row of C: row 8 j + 4 h + i of the instruction is row 16 h + 4 j + i of B.
-// Scale bytes go through LDS too: for every block of 128 (two steps) the word that holds its byte, again for each of its four
-// blocks, so that a pair of steps is free of branches: the compiler moves matrix instructions across those.
+// A workgroup of four waves (2 x 2) computes 64 FM x 64 FN elements of C, each wave FM x FN tiles of 32 x 32, in blocks of 128
+// along the contraction (two instructions deep).  Rows of A and B go from memory straight into LDS, no registers between, 128
+// bytes of a row at a time: whole cache lines (in steps of 64 bytes every line came twice, its first half long gone when the
+// second was asked for: 2.15 against 2.9 PFLOP/s at 8192^3).  Two buffers: block p + 2 is asked for in the second step of
+// block p, when all fragments of p are in registers, and is needed in the second step of p + 1.
+// LDS rows are 128 bytes, eight chunks of 16; chunk c of row r sits at c ^ ((r >> 1) & 7), which keeps the fragment reads (16
+// lanes at a time) free of bank conflicts.  The 32 rows of B of a tile are kept in the order in which the instruction hands its
+// results out, so that a lane ends up with 16 neighbouring elements of a row of C: row 8 j + 4 h + i of the instruction is row
+// 16 h + 4 j + i of B.
+// Scale bytes go through LDS too: for every block the word that holds its byte, again for each of its four blocks, so that
+// the loop is free of branches: the compiler moves matrix instructions across those.
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
@@ -290,8 +293,8 @@ template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt v
 #define TSR_PIN __builtin_amdgcn_sched_barrier(0)
 
 template <int FM, int FN> struct TileLds {
-    static constexpr int ROWS = 64 * (FM + FN), BUF = ROWS * 64, DEPTH = 4;
-    static constexpr int SCALES = DEPTH * BUF, BYTES = SCALES + 4 * ROWS * 4;
+    static constexpr int ROWS = 64 * (FM + FN), BUF = ROWS * 128;
+    static constexpr int SCALES = 2 * BUF, BYTES = SCALES + 2 * ROWS * 4;
 };
 
 template <int FA, int FB, int FM, int FN>
@@ -311,7 +314,7 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void fp8_tile_kernel(co
     const int band = at / (8 * tiles_n), in_band = at - band * 8 * tiles_n, band_rows = min(8, tiles_m - band * 8);
     const int m0 = (band * 8 + in_band % band_rows) * TM, n0 = in_band / band_rows * TN;
 
-    const int k16 = (g.k + 15) & ~15, nk = (g.k + 63) >> 6;
+    const int k16 = (g.k + 15) & ~15, np = (g.k + 127) >> 7;
     const int ma = min(TM, g.a.rows - m0) - 1, nb = min(TN, g.b.rows - n0) - 1;      // last row of each operand's tile
     const i32x4 ra = lds_rsrc(g.a.q + m0 * g.a.ld, ma * g.a.ld + k16);
     const i32x4 rb = lds_rsrc(g.b.q + n0 * g.b.ld, nb * g.b.ld + k16);
@@ -320,21 +323,20 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void fp8_tile_kernel(co
     const i32x4 rsa = lds_rsrc(g.a.scale + sa0 * g.a.ld_scale, (((m0 + ma) >> g.a.shift) - sa0) * g.a.ld_scale + sk);
     const i32x4 rsb = lds_rsrc(g.b.scale + sb0 * g.b.ld_scale, (((n0 + nb) >> g.b.shift) - sb0) * g.b.ld_scale + sk);
 
-    // Loads of a step: wave w brings rows 16 FM w .. of A and 16 FN w .. of B, 16 rows an instruction.  Rows beyond the operand
+    // Loads of a block: wave w brings rows 16 FM w .. of A and 16 FN w .. of B, 8 rows an instruction.  Rows beyond the operand
     // repeat its last one; nothing of them is stored.
     auto n_of = [](int r) { return (r & ~31) + ((r & 4) << 2) + ((r >> 3) & 3) * 4 + (r & 3); };
-    unsigned off[NF];
+    unsigned off[2 * NF];
 #pragma unroll
-    for (int x = 0; x < NF; ++x) {
-        const int r = (x < FM ? wave * 16 * FM + x * 16 : wave * 16 * FN + (x - FM) * 16) + (lane >> 2);
-        const int c = ((lane & 3) ^ ((r >> 1) & 3)) * 16;
-        off[x] = (x < FM ? (unsigned)(min(r, ma) * g.a.ld) : (unsigned)(min(n_of(r), nb) * g.b.ld)) + c;
+    for (int x = 0; x < 2 * NF; ++x) {
+        const int r = (x < 2 * FM ? wave * 16 * FM + x * 8 : wave * 16 * FN + (x - 2 * FM) * 8) + (lane >> 3);
+        const int c = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+        off[x] = (x < 2 * FM ? (unsigned)(min(r, ma) * g.a.ld) : (unsigned)(min(n_of(r), nb) * g.b.ld)) + c;
     }
     const unsigned base = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char*)lds;
-    auto load_one = [&](int t, int x) {                      // part x of step t into its buffer
-        const unsigned to = base + (t & 3) * L::BUF + (x < FM ? wave * 16 * FM + x * 16 : TM + wave * 16 * FN + (x - FM) * 16) * 64;
-        const unsigned v = t < nk ? off[x] + (unsigned)t * 64 : OUT;
-        load_lds16(x < FM ? ra : rb, v, to);
+    auto load_one = [&](int p, int x) {                      // part x of block p into its buffer
+        const unsigned to = base + (p & 1) * L::BUF + (x < 2 * FM ? wave * 16 * FM + x * 8 : TM + wave * 16 * FN + (x - 2 * FM) * 8) * 128;
+        load_lds16(x < 2 * FM ? ra : rb, p < np ? off[x] + (unsigned)p * 128 : OUT, to);
     };
     // Scales of block p: a word for each row of the tile's A rows, then of its B rows; wave w brings 64 SL of them.
     constexpr int SL = (L::ROWS + 255) / 256;
@@ -346,12 +348,11 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void fp8_tile_kernel(co
         soff[x] = r < TM ? (unsigned)((((m0 + min(r, ma)) >> g.a.shift) - sa0) * g.a.ld_scale)
                          : (unsigned)((((n0 + min(n_of(r - TM), nb)) >> g.b.shift) - sb0) * g.b.ld_scale);
     }
-    const int np = (g.k + 127) >> 7;
     auto load_scales = [&](int p) {
 #pragma unroll
         for (int x = 0; x < SL; ++x) {
             const int r = (wave * SL + x) * 64;
-            const unsigned to = base + L::SCALES + ((p & 3) * L::ROWS + r) * 4;
+            const unsigned to = base + L::SCALES + ((p & 1) * L::ROWS + r) * 4;
             load_lds4(r < TM ? rsa : rsb, p < np ? soff[x] + (p & ~3) : OUT, to);
         }
     };
@@ -366,83 +367,75 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void fp8_tile_kernel(co
     i32x8 F[2][NF];
     unsigned sn[NF];
     int s[NF];
-    // where this lane's two chunks of fragment f lie in a buffer
-    const int key = (l32 >> 1) & 3;
-    const int fa = (wm * FM * 32 + l32) * 64, fb = (TM + wn * FN * 32 + l32) * 64;
+    // where this lane's two chunks of fragment f of step slot lie in a buffer: 4 slot + 2 h and the next, by the key of its row
+    const int key = (l32 >> 1) & 7;
+    const int fa = (wm * FM * 32 + l32) * 128, fb = (TM + wn * FN * 32 + l32) * 128;
     const int c0 = ((2 * h) ^ key) * 16, c1 = ((2 * h + 1) ^ key) * 16;
-    auto read = [&](int slot, int t, int f) {
-        const unsigned char* from = lds + (t & 3) * L::BUF + (f < FM ? fa + f * 2048 : fb + (f - FM) * 2048);
-        F[slot][f] = __builtin_shufflevector(*(const i32x4*)(from + c0), *(const i32x4*)(from + c1), 0, 1, 2, 3, 4, 5, 6, 7);
+    auto read = [&](int slot, int p, int f) {
+        const unsigned char* from = lds + (p & 1) * L::BUF + (f < FM ? fa + f * 4096 : fb + (f - FM) * 4096);
+        F[slot][f] = __builtin_shufflevector(*(const i32x4*)(from + (c0 ^ slot * 64)), *(const i32x4*)(from + (c1 ^ slot * 64)), 0, 1, 2, 3, 4, 5, 6, 7);
     };
     auto read_scale = [&](int p, int f) {
         const int r = f < FM ? wm * FM * 32 + f * 32 + l32 : TM + wn * FN * 32 + (f - FM) * 32 + l32;
-        sn[f] = *(const unsigned*)(lds + L::SCALES + ((p & 3) * L::ROWS + r) * 4);
+        sn[f] = *(const unsigned*)(lds + L::SCALES + ((p & 1) * L::ROWS + r) * 4);
     };
 
-    load_scales(0);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        if (t == 2) load_scales(1);
+    for (int p = 0; p < 2; ++p) {
+        load_scales(p);
 #pragma unroll
-        for (int x = 0; x < NF; ++x) load_one(t, x);
+        for (int x = 0; x < 2 * NF; ++x) load_one(p, x);
     }
-    wait_loads<3 * NF + SL>();                               // step 0 and its scales
+    wait_loads<2 * NF + SL>();                               // block 0
     __builtin_amdgcn_s_barrier();
     TSR_PIN;
 #pragma unroll
-    for (int f = 0; f < NF; ++f) read(0, 0, f);
-#pragma unroll
-    for (int f = 0; f < NF; ++f) read_scale(0, f);
+    for (int f = 0; f < NF; ++f) { read(0, 0, f); read_scale(0, f); }
 
-    // Step t (= slot, modulo 2) of block p.  TAIL: what lies beyond k is not part of the sum.
-    auto step = [&](int slot, int p, auto tail) {
+    // Both steps of block p.  TAIL: what lies beyond k is not part of the sum.
+    auto block = [&](int p, auto tail) {
         constexpr bool TAIL = decltype(tail)::value;
-        const int t = 2 * p + slot;
-        // the loads of step t + 1 have landed, everybody's, and everybody has the fragments of step t: in flight may be
-        // what steps t - 1 and t - 2 began
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        wait_loads<2 * NF + SL>();
-        __builtin_amdgcn_s_barrier();
-        TSR_PIN;
-        if (slot == 0) {
 #pragma unroll
-            for (int f = 0; f < NF; ++f) s[f] = (int)(sn[f] >> ((p & 3) * 8));
-            load_scales(p + 2);
-        }
-        if constexpr (TAIL) {
+        for (int slot = 0; slot < 2; ++slot) {
+            if (slot == 0) {
 #pragma unroll
-            for (int f = 0; f < NF; ++f) F[slot][f] = keep_bytes(F[slot][f], g.k - t * 64 - h * 32);
-        }
-        TSR_PIN;
-#pragma unroll
-        for (int q = 0; q < NM; ++q) {
-            const int i = q / FN, j = q % FN;
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(F[slot][FM + j], F[slot][i], acc[i][j], FB, FA, 0, s[FM + j], 0, s[i]);
-            TSR_PIN;
-            // the fragments of the next step (and the scales of the next block) beside the first half, loads beside the second
-            constexpr int HALF = NM / 2;
-            if (q < HALF) {
-#pragma unroll
-                for (int f = q * NF / HALF; f < (q + 1) * NF / HALF; ++f) {
-                    read(slot ^ 1, t + 1, f);
-                    if (slot == 1) read_scale(p + 1, f);
-                }
+                for (int f = 0; f < NF; ++f) s[f] = (int)(sn[f] >> ((p & 3) * 8));
             } else {
+                // block p + 1 has landed, everybody's, and everybody has the fragments of block p
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                wait_loads<0>();
+                __builtin_amdgcn_s_barrier();
+                TSR_PIN;
+                load_scales(p + 2);
+            }
+            if constexpr (TAIL) {
 #pragma unroll
-                for (int x = (q - HALF) * NF / HALF; x < (q - HALF + 1) * NF / HALF; ++x) load_one(t + 4, x);
+                for (int f = 0; f < NF; ++f) F[slot][f] = keep_bytes(F[slot][f], g.k - p * 128 - slot * 64 - h * 32);
             }
             TSR_PIN;
+#pragma unroll
+            for (int q = 0; q < NM; ++q) {
+                const int i = q / FN, j = q % FN;
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(F[slot][FM + j], F[slot][i], acc[i][j], FB, FA, 0, s[FM + j], 0, s[i]);
+                TSR_PIN;
+                // beside the multiplication: the fragments of the next step, and in the second step the loads of block p + 2
+                // and the scales of block p + 1
+#pragma unroll
+                for (int f = q * NF / NM; f < (q + 1) * NF / NM; ++f) {
+                    if (slot == 0) read(1, p, f);
+                    else { read(0, p + 1, f); read_scale(p + 1, f); }
+                }
+                if (slot == 1) {
+#pragma unroll
+                    for (int x = q * 2 * NF / NM; x < (q + 1) * 2 * NF / NM; ++x) load_one(p + 2, x);
+                }
+                TSR_PIN;
+            }
         }
     };
     const int whole = g.k >> 7;
-    for (int p = 0; p < whole; ++p) {
-        step(0, p, std::false_type{});
-        step(1, p, std::false_type{});
-    }
-    if (g.k & 127) {
-        step(0, whole, std::true_type{});
-        step(1, whole, std::true_type{});
-    }
+    for (int p = 0; p < whole; ++p) block(p, std::false_type{});
+    if (g.k & 127) block(whole, std::true_type{});
     wait_loads<0>();                                         // nothing may land after this workgroup's LDS is another's
 
     const bool vec = ((unsigned long long)g.C & 15) == 0 && (g.ldc & 7) == 0;
@@ -469,7 +462,219 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void fp8_tile_kernel(co
     }
 }
 
+// ------------------------------------------------------------------ product, two groups of waves in turn
+// 256 x 256 elements of C by eight waves, 128 x 64 each, in blocks of 128 along the contraction, one workgroup a compute unit
+// that walks its share of the tiles.  Each SIMD holds a wave of either group, and the groups take turns, a barrier between the
+// phases: while one multiplies (32 instructions of 16 x 16 x 128, 1024 cycles) the other moves its fragments of the next
+// block from LDS into registers, so the matrix unit always has a wave that does nothing else.
+//   phase 2 q      group 0 reads block q,        group 1 multiplies block q - 1
+//   phase 2 q + 1  group 0 multiplies block q,   group 1 reads block q
+// In phase 2 q block q + 1 is asked for (A by group 0, B by group 1) into the buffer that block q - 1 has left; it is needed two
+// phases later.  Blocks are counted across tiles: the first block of the next tile is on its way while the last one of this
+// tile is multiplied, and a group writes its part of C while the other multiplies.
+// LDS rows are 128 bytes (whole cache lines), eight chunks of 16; chunk c of row r sits at c ^ ((r >> 1) & 7): 16 lanes that
+// read the same chunk of 16 rows meet no bank twice.  The 64 rows of B of a wave are kept in the order in which the instruction
+// hands its results out: a lane ends up with 16 neighbouring elements of a row of C, 16 lanes apart with a whole line of it.
+// Scale bytes go through LDS as the words that hold them, one for every row and block, again for each of the word's four blocks.
+struct WideLds {
+    static constexpr int BUF = 512 * 128, SCALES = 2 * BUF, BYTES = SCALES + 2 * 512 * 4;
+};
+
+template <int FA, int FB>
+__global__ __launch_bounds__(512, 2) void fp8_wide_kernel(const Fp8Args g) {
+    using L = WideLds;
+    constexpr unsigned OUT = 0x80000000u;                    // an offset beyond every operand: no access
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = wave >> 2, w4 = wave & 3;
+
+    // Tiles: round r of the workgroups takes a run of neighbouring tiles, each XCD (workgroups go round the eight) a run within
+    // it, in bands of 8 rows of tiles, so that the tiles at work on an XCD share rows of A and B in its L2.
+    const int tiles_m = (g.a.rows + 255) >> 8, tiles_n = (g.b.rows + 255) >> 8, tiles = tiles_m * tiles_n;
+    const int first = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    if (first >= tiles) return;
+    auto place = [&](int at, int& m0, int& n0) {
+        const int band = at / (8 * tiles_n), in_band = at - band * 8 * tiles_n, rows = min(8, tiles_m - band * 8);
+        m0 = (band * 8 + in_band % rows) << 8;
+        n0 = (in_band / rows) << 8;
+    };
+    const int k16 = (g.k + 15) & ~15, np = (g.k + 127) >> 7, sk = ((g.k + 511) >> 9) * 4;
+    const int tail = (g.k & 127) ? np - 1 : -1;
+    const unsigned base = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char*)lds;
+
+    // ---- the loader of a group: its operand's 256 rows of the block after the last one it brought, 8 instructions a wave of 8
+    // rows each, and their scales.  Rows beyond the operand repeat its last one; nothing of them is stored.
+    const Fp8Operand& x = group ? g.b : g.a;
+    auto n_of = [](int r) { return (r & ~63) + ((r >> 2) & 3) * 16 + ((r >> 4) & 3) * 4 + (r & 3); };
+    auto again = [](int v) { asm volatile("" : "+v"(v)); return v; };        // what follows from v is not kept in registers
+    auto chunk_of = [&](int lane) { return ((lane & 7) ^ (((w4 * 8 + (lane >> 3)) >> 1) & 7)) * 16; };
+    const int lr = w4 * 8 + (lane >> 3);
+    const unsigned row_off = (unsigned)((group ? n_of(lr) : lr) * x.ld) + chunk_of(lane);
+    const unsigned step0 = (unsigned)x.ld * (group ? 8 : 32), step1 = (unsigned)x.ld * 64;      // from part 2 u to 2 u + 1, to 2 u + 2
+    int l_at = first, l_p = 0, l_buf = 0;
+    i32x4 l_rsrc, l_srsrc;
+    unsigned l_lim, l_soff;
+    auto open_tile = [&]() {
+        int m0, n0;
+        place(min(l_at, tiles - 1), m0, n0);
+        const int x0 = group ? n0 : m0, last = min(256, x.rows - x0) - 1, s0 = x0 >> x.shift;
+        l_rsrc = lds_rsrc(x.q + x0 * x.ld, last * x.ld + k16);
+        const int ln = again(lane), sr = group ? n_of(w4 * 64 + ln) : w4 * 64 + ln;
+        l_lim = (unsigned)(last * x.ld) + chunk_of(ln);
+        l_srsrc = lds_rsrc(x.scale + s0 * x.ld_scale, (((x0 + last) >> x.shift) - s0) * x.ld_scale + sk);
+        l_soff = (unsigned)((((x0 + min(sr, last)) >> x.shift) - s0) * x.ld_scale);
+    };
+    auto load_part = [&](int u) {                            // u < 8: rows; 8: scales
+        const bool live = l_at < tiles;
+        if (u < 8) {
+            const unsigned r = min((unsigned)again((int)row_off) + (unsigned)(u >> 1) * step1 + (unsigned)(u & 1) * step0, l_lim);
+            load_lds16(l_rsrc, live ? r + (unsigned)l_p * 128 : OUT, base + l_buf * L::BUF + (group * 256 + u * 32 + w4 * 8) * 128);
+        } else {
+            load_lds4(l_srsrc, live ? l_soff + (l_p & ~3) : OUT, base + L::SCALES + (l_buf * 512 + group * 256 + w4 * 64) * 4);
+        }
+    };
+    auto next_block = [&]() {
+        l_buf ^= 1;
+        if (++l_p == np) { l_p = 0; l_at += gridDim.x; open_tile(); }
+    };
+
+    // ---- fragments: 32 bytes a lane, chunks 2 quad and 2 quad + 1 of its row
+    i32x8 A[8], B[4];
+    int sa[2], sb;
+    auto read = [&](int buf, int p) {
+        const int ln = again(lane), row = ln & 15, row_a = group * 128 + row, row_b = 256 + w4 * 64 + row;
+        const int c0 = ((2 * (ln >> 4)) ^ ((row >> 1) & 7)) * 16, c1 = c0 ^ 16;
+        const unsigned char* sc = lds + L::SCALES + buf * 2048 + (p & 3);
+        const unsigned char* at = lds + buf * L::BUF;
+        auto fetch = [&](const unsigned char* from) {
+            return __builtin_shufflevector(*(const i32x4*)(from + c0), *(const i32x4*)(from + c1), 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        auto four = [&](int row) {
+            return (int)(sc[row * 4] | sc[(row + 16) * 4] << 8 | sc[(row + 32) * 4] << 16 | (unsigned)sc[(row + 48) * 4] << 24);
+        };
+        sa[0] = four(row_a); sa[1] = four(row_a + 64); sb = four(row_b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) B[j] = fetch(at + (row_b + j * 16) * 128);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) A[i] = fetch(at + (row_a + i * 16) * 128);
+        if (p == tail) {                                     // what lies beyond k is not part of the sum
+            const int valid = g.k - p * 128 - (ln >> 4) * 32;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) B[j] = keep_bytes(B[j], valid);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) A[i] = keep_bytes(A[i], valid);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
+    f32x4 acc[8][4];
+    auto clear = [&]() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    };
+    // the four products of row group i
+#define TSR_MUL(i, j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(B[j], A[i], acc[i][j], FB, FA, j, sb, (i) & 3, sa[(i) >> 2])
+#define TSR_MUL4(i) TSR_MUL(i, 0); TSR_MUL(i, 1); TSR_MUL(i, 2); TSR_MUL(i, 3); TSR_PIN
+    auto hold = [&]() {                                      // the products are done here, not where the compiler would move them
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            asm volatile("" : "+v"(acc[i][0]), "+v"(acc[i][1]), "+v"(acc[i][2]), "+v"(acc[i][3]));
+    };
+    const bool vec = ((unsigned long long)g.C & 15) == 0 && (g.ldc & 7) == 0;
+    auto store = [&](int at) {
+        int m0, n0;
+        place(at, m0, n0);
+        const int ln = again(lane), n = n0 + w4 * 64 + (ln >> 4) * 16;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int m = m0 + group * 128 + i * 16 + (ln & 15);
+            typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+            bf16x8 lo, hi;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { lo[e] = (__bf16)acc[i][e >> 2][e & 3]; hi[e] = (__bf16)acc[i][2 + (e >> 2)][e & 3]; }
+            if (m >= g.a.rows) continue;
+            __bf16* to = (__bf16*)g.C + (long long)m * g.ldc + n;
+            if (vec && n + 16 <= g.b.rows) {
+                *(bf16x8*)to = lo;
+                *(bf16x8*)(to + 8) = hi;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) if (n + e < g.b.rows) to[e] = e < 8 ? lo[e & 7] : hi[e & 7];
+            }
+        }
+    };
+    auto phase_end = [&]() { TSR_PIN; __builtin_amdgcn_s_barrier(); TSR_PIN; };
+
+    open_tile();
+#pragma unroll
+    for (int u = 0; u < 9; ++u) load_part(u);
+    wait_loads<0>();
+    phase_end();
+    next_block();
+    int buf = 0;
+    clear();
+    if (group == 0) {
+        for (int at = first; at < tiles; at += gridDim.x) {
+            for (int p = 0; p < np; ++p) {
+#pragma unroll
+                for (int u = 0; u < 9; ++u) load_part(u);
+                read(buf, p);
+                next_block();
+                buf ^= 1;
+                phase_end();
+                __builtin_amdgcn_s_setprio(1);
+                TSR_MUL4(0); TSR_MUL4(1); TSR_MUL4(2); TSR_MUL4(3); TSR_MUL4(4); TSR_MUL4(5); TSR_MUL4(6); TSR_MUL4(7);
+                __builtin_amdgcn_s_setprio(0);
+                hold();
+                wait_loads<0>();
+                phase_end();
+            }
+            store(at);
+            clear();
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < 9; ++u) load_part(u);
+        next_block();
+        phase_end();
+        for (int at = first; at < tiles; at += gridDim.x) {
+            for (int p = 0; p < np; ++p) {
+                read(buf, p);
+                wait_loads<0>();
+                buf ^= 1;
+                phase_end();
+                __builtin_amdgcn_s_setprio(1);
+                TSR_MUL4(0); load_part(0); TSR_PIN;
+                TSR_MUL4(1); load_part(1); load_part(8); TSR_PIN;
+                TSR_MUL4(2); load_part(2); TSR_PIN;
+                TSR_MUL4(3); load_part(3); TSR_PIN;
+                TSR_MUL4(4); load_part(4); TSR_PIN;
+                TSR_MUL4(5); load_part(5); TSR_PIN;
+                TSR_MUL4(6); load_part(6); TSR_PIN;
+                TSR_MUL4(7); load_part(7); TSR_PIN;
+                __builtin_amdgcn_s_setprio(0);
+                hold();
+                next_block();
+                if (at + (int)gridDim.x < tiles || p + 1 < np) phase_end();
+            }
+            store(at);
+            clear();
+        }
+        wait_loads<0>();
+    }
+#undef TSR_MUL
+#undef TSR_MUL4
+}
+
 template <int FA, int FB> hipError_t launch_tiles(const Fp8Args& a, int shape, hipStream_t stream) {
+    if (shape == 0) {
+        const long long tiles = (long long)((a.a.rows + 255) / 256) * ((a.b.rows + 255) / 256);
+        const hipError_t e = allow_lds((const void*)fp8_wide_kernel<FA, FB>, WideLds::BYTES);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((fp8_wide_kernel<FA, FB>), dim3((unsigned)(tiles < 256 ? (tiles + 7) / 8 * 8 : 256)), dim3(512), WideLds::BYTES, stream, a);
+        return hipGetLastError();
+    }
     const int t = shape == 0 ? 256 : 128;
     const long long tiles = (long long)((a.a.rows + t - 1) / t) * ((a.b.rows + t - 1) / t);
     const int bytes = shape == 0 ? TileLds<4, 4>::BYTES : TileLds<2, 2>::BYTES;

@@ -156,6 +156,21 @@ def test_matmul(tsr, m, n, k, ta, tb, ra, rb, pitch):
     check_product(tsr, ops, m, n, k, pitch)
 
 
+@pytest.mark.parametrize("m,n,k", [(4100, 4000, 136), (4096, 4096, 384), (8200, 3900, 100), (2049, 16400, 513)])
+def test_matmul_of_many_tiles(tsr, m, n, k):
+    """More tiles than compute units, ragged at the right and the bottom; the result against fp64 on the GPU."""
+    ops = product_case(tsr, m, n, k, E5, E4, 1, 128, m)
+    C = torch.full((m, n), 3.0, device="cuda", dtype=torch.bfloat16)
+    tsr.tsr_fp8_matmul(*ops, C)
+    torch.cuda.synchronize()
+    a, b = values(ops[0], ops[1], k).cuda(), values(ops[2], ops[3], k).cuda()
+    want = a @ b.t()
+    bound = ((7 * 2.0 ** -13 + (k + 8) * 2.0 ** -23) * (a.abs() @ b.abs().t()) + 1e-40) * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs()      # as in check_product
+    err = (C.double() - want).abs()
+    assert bool((err <= bound).all()), (err / bound).max().item()
+    assert torch.linalg.norm(C.double() - want) <= (2.0 ** -8 + 2.0 ** -12) * torch.linalg.norm(want)
+
+
 def test_matmul_values_that_show_a_wrong_place(tsr):
     """Whole numbers: every element of the result is exact, so a misplaced row, column or scale shows."""
     m, n, k = 70, 90, 300
