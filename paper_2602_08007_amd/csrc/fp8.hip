@@ -530,7 +530,7 @@ __global__ __launch_bounds__(512, 2) void fp8_wide_kernel(const Fp8Args g) {
             const unsigned r = min((unsigned)again((int)row_off) + (unsigned)(u >> 1) * step1 + (unsigned)(u & 1) * step0, l_lim);
             load_lds16(l_rsrc, live ? r + (unsigned)l_p * 128 : OUT, base + l_buf * L::BUF + (group * 256 + u * 32 + w4 * 8) * 128);
         } else {
-            load_lds4(l_srsrc, live ? l_soff + (l_p & ~3) : OUT, base + L::SCALES + (l_buf * 512 + group * 256 + w4 * 64) * 4);
+            load_lds4(l_srsrc, live && (l_p & 3) == 0 ? l_soff + l_p : OUT, base + L::SCALES + (l_buf * 512 + group * 256 + w4 * 64) * 4);
         }
     };
     auto next_block = [&]() {
@@ -540,19 +540,26 @@ __global__ __launch_bounds__(512, 2) void fp8_wide_kernel(const Fp8Args g) {
 
     // ---- fragments: 32 bytes a lane, chunks 2 quad and 2 quad + 1 of its row
     i32x8 A[8], B[4];
-    int sa[2], sb;
+    int sa[8], sb[4];                                        // scales: this block's byte lowest, those of the word's later blocks above
     auto read = [&](int buf, int p) {
         const int ln = again(lane), row = ln & 15, row_a = group * 128 + row, row_b = 256 + w4 * 64 + row;
         const int c0 = ((2 * (ln >> 4)) ^ ((row >> 1) & 7)) * 16, c1 = c0 ^ 16;
-        const unsigned char* sc = lds + L::SCALES + buf * 2048 + (p & 3);
         const unsigned char* at = lds + buf * L::BUF;
         auto fetch = [&](const unsigned char* from) {
             return __builtin_shufflevector(*(const i32x4*)(from + c0), *(const i32x4*)(from + c1), 0, 1, 2, 3, 4, 5, 6, 7);
         };
-        auto four = [&](int row) {
-            return (int)(sc[row * 4] | sc[(row + 16) * 4] << 8 | sc[(row + 32) * 4] << 16 | (unsigned)sc[(row + 48) * 4] << 24);
-        };
-        sa[0] = four(row_a); sa[1] = four(row_a + 64); sb = four(row_b);
+        if ((p & 3) == 0) {
+            const unsigned char* sc = lds + L::SCALES + buf * 2048;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sb[j] = *(const int*)(sc + (row_b + j * 16) * 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sa[i] = *(const int*)(sc + (row_a + i * 16) * 4);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sb[j] = (int)((unsigned)sb[j] >> 8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sa[i] = (int)((unsigned)sa[i] >> 8);
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) B[j] = fetch(at + (row_b + j * 16) * 128);
 #pragma unroll
@@ -564,8 +571,8 @@ __global__ __launch_bounds__(512, 2) void fp8_wide_kernel(const Fp8Args g) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) A[i] = keep_bytes(A[i], valid);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
+    auto wait_reads = []() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
     f32x4 acc[8][4];
     auto clear = [&]() {
 #pragma unroll
@@ -573,14 +580,31 @@ __global__ __launch_bounds__(512, 2) void fp8_wide_kernel(const Fp8Args g) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     };
-    // the four products of row group i
-#define TSR_MUL(i, j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(B[j], A[i], acc[i][j], FB, FA, j, sb, (i) & 3, sa[(i) >> 2])
-#define TSR_MUL4(i) TSR_MUL(i, 0); TSR_MUL(i, 1); TSR_MUL(i, 2); TSR_MUL(i, 3); TSR_PIN
-    auto hold = [&]() {                                      // the products are done here, not where the compiler would move them
+    auto phase_end = [&]() { TSR_PIN; __builtin_amdgcn_s_barrier(); TSR_PIN; };
+    // the 32 products of a block, with a group's loads among them (LOADS) or not
+    auto multiply = [&](auto loads) {
+        constexpr bool LOADS = decltype(loads)::value;
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(B[j], A[i], acc[i][j], FB, FA, 0, sb[j], 0, sa[i]);
+            TSR_PIN;
+            if constexpr (LOADS) {
+                load_part(i);
+                if (i == 3) load_part(8);
+                TSR_PIN;
+            }
+        }
+        __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)                          // the products are done here, not where the compiler would move them
             asm volatile("" : "+v"(acc[i][0]), "+v"(acc[i][1]), "+v"(acc[i][2]), "+v"(acc[i][3]));
     };
+    // A result that the 256 MB of the last cache cannot hold is written past the caches (8192 x 32000 x 2048: 495 -> 482 us); a
+    // smaller one is left there for whoever reads it next (8192 x 8192 x 2048: 124 us, and 136 past the caches).
+    const bool large = (long long)g.a.rows * g.b.rows > (128ll << 20);
     const bool vec = ((unsigned long long)g.C & 15) == 0 && (g.ldc & 7) == 0;
     auto store = [&](int at) {
         int m0, n0;
@@ -596,16 +620,19 @@ __global__ __launch_bounds__(512, 2) void fp8_wide_kernel(const Fp8Args g) {
             if (m >= g.a.rows) continue;
             __bf16* to = (__bf16*)g.C + (long long)m * g.ldc + n;
             if (vec && n + 16 <= g.b.rows) {
-                *(bf16x8*)to = lo;
-                *(bf16x8*)(to + 8) = hi;
+                if (large) {
+                    __builtin_nontemporal_store(lo, (bf16x8*)to);
+                    __builtin_nontemporal_store(hi, (bf16x8*)(to + 8));
+                } else {
+                    *(bf16x8*)to = lo;
+                    *(bf16x8*)(to + 8) = hi;
+                }
             } else {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) if (n + e < g.b.rows) to[e] = e < 8 ? lo[e & 7] : hi[e & 7];
             }
         }
     };
-    auto phase_end = [&]() { TSR_PIN; __builtin_amdgcn_s_barrier(); TSR_PIN; };
-
     open_tile();
 #pragma unroll
     for (int u = 0; u < 9; ++u) load_part(u);
@@ -617,22 +644,22 @@ __global__ __launch_bounds__(512, 2) void fp8_wide_kernel(const Fp8Args g) {
     if (group == 0) {
         for (int at = first; at < tiles; at += gridDim.x) {
             for (int p = 0; p < np; ++p) {
+                read(buf, p);
+                TSR_PIN;
 #pragma unroll
                 for (int u = 0; u < 9; ++u) load_part(u);
-                read(buf, p);
                 next_block();
                 buf ^= 1;
+                wait_reads();
                 phase_end();
-                __builtin_amdgcn_s_setprio(1);
-                TSR_MUL4(0); TSR_MUL4(1); TSR_MUL4(2); TSR_MUL4(3); TSR_MUL4(4); TSR_MUL4(5); TSR_MUL4(6); TSR_MUL4(7);
-                __builtin_amdgcn_s_setprio(0);
-                hold();
+                multiply(std::false_type{});
                 wait_loads<0>();
                 phase_end();
             }
             store(at);
             clear();
         }
+        phase_end();                                         // group 1 is a phase behind
     } else {
 #pragma unroll
         for (int u = 0; u < 9; ++u) load_part(u);
@@ -641,30 +668,19 @@ __global__ __launch_bounds__(512, 2) void fp8_wide_kernel(const Fp8Args g) {
         for (int at = first; at < tiles; at += gridDim.x) {
             for (int p = 0; p < np; ++p) {
                 read(buf, p);
-                wait_loads<0>();
                 buf ^= 1;
+                wait_reads();
+                wait_loads<0>();
                 phase_end();
-                __builtin_amdgcn_s_setprio(1);
-                TSR_MUL4(0); load_part(0); TSR_PIN;
-                TSR_MUL4(1); load_part(1); load_part(8); TSR_PIN;
-                TSR_MUL4(2); load_part(2); TSR_PIN;
-                TSR_MUL4(3); load_part(3); TSR_PIN;
-                TSR_MUL4(4); load_part(4); TSR_PIN;
-                TSR_MUL4(5); load_part(5); TSR_PIN;
-                TSR_MUL4(6); load_part(6); TSR_PIN;
-                TSR_MUL4(7); load_part(7); TSR_PIN;
-                __builtin_amdgcn_s_setprio(0);
-                hold();
+                multiply(std::true_type{});
                 next_block();
-                if (at + (int)gridDim.x < tiles || p + 1 < np) phase_end();
+                phase_end();
             }
             store(at);
             clear();
         }
-        wait_loads<0>();
+        wait_loads<0>();                                     // nothing may land after this workgroup's LDS is another's
     }
-#undef TSR_MUL
-#undef TSR_MUL4
 }
 
 template <int FA, int FB> hipError_t launch_tiles(const Fp8Args& a, int shape, hipStream_t stream) {
