@@ -391,7 +391,8 @@ int tsr_fp8_quantize(const void* X, int x_dtype, int m, int n, long long ldx, in
  * A and B aligned as above; the bytes from a row's k values to the next multiple of 16, and from its scales to the next
  * multiple of 4, may be read but do not count.  m and n as they are, k up to 2^22.  C needs the alignment of its type only
  * and must not overlap A, B or their scales.
- * Workspace: tsr_fp8_matmul_workspace_bytes (0 where the product needs none: ws may then be NULL). */
+ * Workspace: tsr_fp8_matmul_workspace_bytes, 0 for most sizes; where a small result is cut along k, a smaller workspace
+ * means fewer pieces, and NULL none. */
 typedef struct tsr_fp8_matrix {
     const void* q;
     const unsigned char* scale;

@@ -459,13 +459,20 @@ def _device_of(*tensors) -> torch.device:
 
 def _launch(dev: torch.device, stream, fn, *args) -> None:
     """fn(*args, stream) with the tensors' device current; the stream is that device's current one unless given."""
-    if isinstance(stream, torch.cuda.Stream) and stream.device != dev:
-        raise ValueError("the stream belongs to another device than the tensors")
-    if dev.index == torch.cuda.current_device():
-        _check(fn(*args, _stream(stream)))
+    at = dev.index
+    if stream is None:
+        handle = torch.cuda.current_stream(at).cuda_stream
+    else:
+        if isinstance(stream, torch.cuda.Stream) and stream.device != dev:
+            raise ValueError("the stream belongs to another device than the tensors")
+        handle = _stream(stream)
+    if at == torch.cuda.current_device():
+        status = fn(*args, handle)
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, _stream(stream)))
+            status = fn(*args, handle)
+    if status:
+        raise TsrError(status)
 
 
 class TensorSet:
@@ -578,9 +585,11 @@ def _fp8_place(q, s, rows, cols, block_rows, name):
 
 def _rows_ld(t: torch.Tensor) -> int:
     """Leading dimension; that of a single column or row may be anything in torch, and is made one that holds the row."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    rows, cols = t.shape
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
         raise TypeError("expected a row-major 2-D tensor (unit column stride)")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), -(-t.shape[1] // 16) * 16)
+    return ld if rows > 1 else max(ld, -(-cols // 16) * 16)
 
 
 def tsr_fp8_quantize(X, Q=None, S=None, Qt=None, St=None, block_rows=1, stream=None):
@@ -597,9 +606,13 @@ def tsr_fp8_quantize(X, Q=None, S=None, Qt=None, St=None, block_rows=1, stream=N
 
 def _fp8_operand(q, s, k, name) -> tsr_fp8_matrix:
     rows = q.shape[0]
-    if s.dtype != torch.uint8 or s.dim() != 2 or s.shape[1] != -(-k // 128) or s.shape[0] not in (rows, -(-rows // 128)):
+    srows, scols = s.shape
+    dtype = _FP8.get(q.dtype)
+    if dtype is None:
+        raise TypeError("%s must be float8_e4m3fn or float8_e5m2" % name)
+    if s.dtype != torch.uint8 or scols != -(-k // 128) or srows not in (rows, -(-rows // 128)):
         raise ValueError("the scales of %s must be uint8, one for each 128 values of a row or of 128 rows" % name)
-    return tsr_fp8_matrix(_ptr(q), _ptr(s), _rows_ld(q), _rows_ld(s), _fp8(q), 1 if s.shape[0] == rows else 128)
+    return tsr_fp8_matrix(q.data_ptr(), s.data_ptr(), _rows_ld(q), _rows_ld(s), dtype, 1 if srows == rows else 128)
 
 
 def tsr_fp8_matmul_workspace_bytes(m: int, n: int, k: int) -> int:

@@ -22,7 +22,16 @@ struct Fp8Args {
     Fp8Operand a, b;            // C is a.rows x b.rows
     int k;
     void* C; long long ldc;     // bf16
+    // set by the launch
+    float* partial; long long ldp;       // pieces of the contraction: fp32 sums of each, rows of ldp
+    int chunk;                           // of k in a piece, a multiple of 512
+    int groups_n;                        // of 16 rows of B
 };
-hipError_t launch_fp8_matmul(const Fp8Args& a, int fmt_a, int fmt_b, hipStream_t stream);
+
+// How a product is done, by its sizes alone.
+enum { FP8_DIRECT = 0, FP8_TILES = 1, FP8_WIDE = 2 };
+struct Fp8Plan { int kind, pieces; long long ldp; };
+Fp8Plan fp8_plan(int m, int n, int k);
+hipError_t launch_fp8_matmul(const Fp8Args& a, const Fp8Plan& p, int fmt_a, int fmt_b, hipStream_t stream);
 
 }  // namespace tsr

@@ -48,7 +48,8 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
     __shared__ __attribute__((aligned(16))) unsigned char turned[128 * PITCH];
     __shared__ unsigned col_max[4][128];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int row0 = blockIdx.y * 128, col0 = blockIdx.x * 128;
+    const int tiles_n = (a.n + 127) >> 7, tile_m = blockIdx.x / tiles_n, tile_n = blockIdx.x - tile_m * tiles_n;
+    const int row0 = tile_m * 128, col0 = tile_n * 128;
     const int r0 = row0 + (tid >> 4) * 8, c0 = col0 + (tid & 15) * 8;
     float x[8][8];
 #pragma unroll
@@ -125,13 +126,13 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
                 else
 #pragma unroll
                     for (int j = 0; j < 8; ++j) if (c0 + j < a.n) to[j] = (unsigned char)(q[j >> 2] >> (8 * (j & 3)));
-                if (ROWS == 1 && (tid & 15) == 0) a.S[(long long)(r0 + i) * a.lds + blockIdx.x] = (unsigned char)b;
+                if (ROWS == 1 && (tid & 15) == 0) a.S[(long long)(r0 + i) * a.lds + tile_n] = (unsigned char)b;
             }
         }
     }
     if (ROWS == 128 && tid == 0) {
-        if (a.Q) a.S[(long long)blockIdx.y * a.lds + blockIdx.x] = (unsigned char)tile_byte;
-        if (a.Qt) a.St[(long long)blockIdx.x * a.ldst + blockIdx.y] = (unsigned char)tile_byte;
+        if (a.Q) a.S[(long long)tile_m * a.lds + tile_n] = (unsigned char)tile_byte;
+        if (a.Qt) a.St[(long long)tile_n * a.ldst + tile_m] = (unsigned char)tile_byte;
     }
     if (!a.Qt) return;
 #pragma unroll
@@ -143,7 +144,7 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
         for (int i = 0; i < 8; ++i) y[i] = x[i][j] * inv;
         const u32x2 q = {fp8_encode4<FMT>(y), fp8_encode4<FMT>(y + 4)};
         *(u32x2*)(turned + ((tid & 15) * 8 + j) * PITCH + (tid >> 4) * 8) = q;
-        if (ROWS == 1 && tid < 16 && c0 + j < a.n) a.St[(long long)(c0 + j) * a.ldst + blockIdx.y] = (unsigned char)b;
+        if (ROWS == 1 && tid < 16 && c0 + j < a.n) a.St[(long long)(c0 + j) * a.ldst + tile_m] = (unsigned char)b;
     }
     __syncthreads();
 #pragma unroll
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
 }
 
 hipError_t launch_fp8_quantize(const QuantizeArgs& a, int fmt, int block_rows, hipStream_t stream) {
-    const dim3 grid((unsigned)((a.n + 127) / 128), (unsigned)((a.m + 127) / 128));
+    const dim3 grid((unsigned)(((a.n + 127ll) / 128) * ((a.m + 127ll) / 128)));
 #define TSR_Q(F, R, X) hipLaunchKernelGGL((fp8_quantize_kernel<F, R, X>), grid, dim3(256), 0, stream, a)
     const int v = (fmt == FP8_E5M2 ? 4 : 0) + (block_rows == 128 ? 2 : 0) + (a.x_bf16 ? 1 : 0);
     switch (v) {
@@ -204,7 +205,7 @@ template <int FA, int FB, int FM>
 __global__ __launch_bounds__(256) void fp8_direct_kernel(const Fp8Args g) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int l16 = lane & 15, quad = lane >> 4;
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * (16 * FM);
+    const int n0 = blockIdx.x % g.groups_n * 16, m0 = blockIdx.x / g.groups_n * (16 * FM);
     const int k16 = (g.k + 15) & ~15, blocks = (g.k + 127) >> 7;
     const int brow = min(n0 + l16, g.b.rows - 1);
     const rsrc_t rb = make_rsrc(g.b.q + n0 * g.b.ld, (long long)(min(16, g.b.rows - n0) - 1) * g.b.ld + k16);
@@ -227,23 +228,36 @@ __global__ __launch_bounds__(256) void fp8_direct_kernel(const Fp8Args g) {
     f32x4 acc[FM];
 #pragma unroll
     for (int f = 0; f < FM; ++f) acc[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int kb = wave; kb < blocks; kb += 4) {
-        const unsigned k0 = (unsigned)kb * 128;
-        i32x8 b = fetch(rb, ob + k0), x[FM];
-        const int scale_b = sb[kb];
-        int scale_a[FM];
+    // N blocks of this wave from kb on: all loads first, so that a few hundred rows of B keep the memory busy
+    auto blocks_from = [&](int kb, auto number) {
+        constexpr int N = decltype(number)::value;
+        i32x8 b[N], x[N][FM];
+        int scale_b[N], scale_a[N][FM];
 #pragma unroll
-        for (int f = 0; f < FM; ++f) { x[f] = fetch(ra, oa[f] + k0); scale_a[f] = sa[f][kb]; }
-        const int valid = g.k - (int)k0 - quad * 32;
-        if (g.k - (int)k0 < 128) {
-            b = keep_bytes(b, valid);
+        for (int u = 0; u < N; ++u) {
+            const unsigned k0 = (unsigned)(kb + 4 * u) * 128;
+            b[u] = fetch(rb, ob + k0);
+            scale_b[u] = sb[kb + 4 * u];
 #pragma unroll
-            for (int f = 0; f < FM; ++f) x[f] = keep_bytes(x[f], valid);
+            for (int f = 0; f < FM; ++f) { x[u][f] = fetch(ra, oa[f] + k0); scale_a[u][f] = sa[f][kb + 4 * u]; }
         }
 #pragma unroll
-        for (int f = 0; f < FM; ++f)
-            acc[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, x[f], acc[f], FB, FA, 0, scale_b, 0, scale_a[f]);
-    }
+        for (int u = 0; u < N; ++u) {
+            const int left = g.k - (kb + 4 * u) * 128;
+            if (left < 128) {
+                b[u] = keep_bytes(b[u], left - quad * 32);
+#pragma unroll
+                for (int f = 0; f < FM; ++f) x[u][f] = keep_bytes(x[u][f], left - quad * 32);
+            }
+#pragma unroll
+            for (int f = 0; f < FM; ++f)
+                acc[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[u], x[u][f], acc[f], FB, FA, 0, scale_b[u], 0, scale_a[u][f]);
+        }
+    };
+    constexpr int AHEAD = FM == 1 ? 4 : 2;
+    int kb = wave;
+    for (; kb + 4 * (AHEAD - 1) < blocks; kb += 4 * AHEAD) blocks_from(kb, std::integral_constant<int, AHEAD>{});
+    for (; kb < blocks; kb += 4) blocks_from(kb, std::integral_constant<int, 1>{});
     __shared__ __attribute__((aligned(16))) f32x4 part[4][FM][64];
 #pragma unroll
     for (int f = 0; f < FM; ++f) part[wave][f][lane] = acc[f];
@@ -297,8 +311,14 @@ template <int FM, int FN> struct TileLds {
     static constexpr int SCALES = 2 * BUF, BYTES = SCALES + 2 * ROWS * 4;
 };
 
+// With more than one piece (blockIdx.y) of the contraction each writes its fp32 sums, and fp8_join_kernel adds them up.
 template <int FA, int FB, int FM, int FN>
-__global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void fp8_tile_kernel(const Fp8Args g) {
+__global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void fp8_tile_kernel(const Fp8Args whole_k) {
+    Fp8Args g = whole_k;
+    const long long k_from = (long long)blockIdx.y * g.chunk;
+    g.a.q += k_from; g.b.q += k_from;
+    g.a.scale += k_from >> 7; g.b.scale += k_from >> 7;
+    g.k = (int)min((long long)g.chunk, g.k - k_from);
     using L = TileLds<FM, FN>;
     constexpr int TM = 64 * FM, TN = 64 * FN, NF = FM + FN, NM = FM * FN;
     constexpr unsigned OUT = 0x80000000u;                    // an offset beyond every operand: no access
@@ -438,6 +458,22 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void fp8_tile_kernel(co
     if (g.k & 127) block(whole, std::true_type{});
     wait_loads<0>();                                         // nothing may land after this workgroup's LDS is another's
 
+    if (g.partial) {
+        float* part = g.partial + (long long)blockIdx.y * g.a.rows * g.ldp;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int m = m0 + wm * FM * 32 + i * 32 + l32;
+            if (m >= g.a.rows) continue;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const int n = n0 + wn * FN * 32 + j * 32 + h * 16 + e;
+                    if (n < g.b.rows) *(f32x4*)(part + (long long)m * g.ldp + n) = f32x4{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+                }
+        }
+        return;
+    }
     const bool vec = ((unsigned long long)g.C & 15) == 0 && (g.ldc & 7) == 0;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
@@ -683,40 +719,83 @@ __global__ __launch_bounds__(512, 2) void fp8_wide_kernel(const Fp8Args g) {
     }
 }
 
-template <int FA, int FB> hipError_t launch_tiles(const Fp8Args& a, int shape, hipStream_t stream) {
-    if (shape == 0) {
-        const long long tiles = (long long)((a.a.rows + 255) / 256) * ((a.b.rows + 255) / 256);
+// The sum of the pieces, in their order, as bf16.
+__global__ __launch_bounds__(256) void fp8_join_kernel(const Fp8Args g, int pieces) {
+    const long long quads = g.ldp >> 2, at = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (at >= quads * g.a.rows) return;
+    const long long m = at / quads;
+    const int n = (int)(at - m * quads) * 4;
+    const float* from = g.partial + m * g.ldp + n;
+    f32x4 sum = *(const f32x4*)from;
+    for (int p = 1; p < pieces; ++p) sum += *(const f32x4*)(from + (long long)p * g.a.rows * g.ldp);
+    __bf16* to = (__bf16*)g.C + m * g.ldc + n;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) if (n + e < g.b.rows) to[e] = (__bf16)sum[e];
+}
+
+namespace {
+long long tiles_of(int m, int n, int t) { return ((m + t - 1ll) / t) * ((n + t - 1ll) / t); }
+}
+
+Fp8Plan fp8_plan(int m, int n, int k) {
+    Fp8Plan p{};
+    p.pieces = 1;
+    p.ldp = (n + 3) & ~3ll;
+    // few rows or columns: bound by reading the other operand (32 x 5461 x 2048: 8.8 us, in tiles 10.4; 64 rows: 13.8 and 11.5)
+    if (m <= 32 || n <= 32) { p.kind = FP8_DIRECT; return p; }
+    // 160 tiles of 256 x 256 keep enough compute units busy (2048 x 5461 x 16384, 176 tiles: 224 us, in 128 x 128 241 us; 2048 x
+    // 4096 x 2048, 128 tiles: 31 and 23 us)
+    if (tiles_of(m, n, 256) >= 160) { p.kind = FP8_WIDE; return p; }
+    p.kind = FP8_TILES;
+    // Pieces of the contraction, at least 512 each: what the time in us is, as measured from 512 x 512 x 8192 (31 us whole, 16.5 in
+    // four) over 768 x 768 x 16384 (80; 28 in six) and 2736 x 1024 x 12345 (78; 68 in two) to 2048 x 2048 x 2048 (14; 35 in two):
+    // 4.5 ns for every step along k while the tiles fit the card at once, and for pieces a second launch and their sums
+    // written and read at 3 TB/s.
+    const double tiles = (double)tiles_of(m, n, 128);
+    double least = 0.0;
+    for (int s = 1; s <= 16 && (s == 1 || k / s >= 512); ++s) {
+        const double busy = tiles * s / 300.0;
+        const double us = k * 0.0045 * (busy > 1.0 ? busy : 1.0) / s + (s == 1 ? 0.0 : 3.0 + s * (double)m * n * 8.0 / 3e6);
+        if (s == 1 || us < least) { least = us; p.pieces = s; }
+    }
+    return p;
+}
+
+template <int FA, int FB> hipError_t launch_kind(Fp8Args a, const Fp8Plan& p, hipStream_t stream) {
+    if (p.kind == FP8_DIRECT) {
+        const int fm = a.a.rows <= 16 ? 1 : a.a.rows <= 32 ? 2 : 4;
+        a.groups_n = (int)((a.b.rows + 15ll) / 16);
+        const dim3 grid((unsigned)((long long)a.groups_n * ((a.a.rows + 16 * fm - 1) / (16 * fm))));
+        if (fm == 1) hipLaunchKernelGGL((fp8_direct_kernel<FA, FB, 1>), grid, dim3(256), 0, stream, a);
+        else if (fm == 2) hipLaunchKernelGGL((fp8_direct_kernel<FA, FB, 2>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((fp8_direct_kernel<FA, FB, 4>), grid, dim3(256), 0, stream, a);
+        return hipGetLastError();
+    }
+    if (p.kind == FP8_WIDE) {
+        const long long tiles = tiles_of(a.a.rows, a.b.rows, 256);
         const hipError_t e = allow_lds((const void*)fp8_wide_kernel<FA, FB>, WideLds::BYTES);
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL((fp8_wide_kernel<FA, FB>), dim3((unsigned)(tiles < 256 ? (tiles + 7) / 8 * 8 : 256)), dim3(512), WideLds::BYTES, stream, a);
         return hipGetLastError();
     }
-    const int t = shape == 0 ? 256 : 128;
-    const long long tiles = (long long)((a.a.rows + t - 1) / t) * ((a.b.rows + t - 1) / t);
-    const int bytes = shape == 0 ? TileLds<4, 4>::BYTES : TileLds<2, 2>::BYTES;
-    const void* k = shape == 0 ? (const void*)fp8_tile_kernel<FA, FB, 4, 4> : (const void*)fp8_tile_kernel<FA, FB, 2, 2>;
-    const hipError_t e = allow_lds(k, bytes);
+    const hipError_t e = allow_lds((const void*)fp8_tile_kernel<FA, FB, 2, 2>, TileLds<2, 2>::BYTES);
     if (e != hipSuccess) return e;
-    if (shape == 0) hipLaunchKernelGGL((fp8_tile_kernel<FA, FB, 4, 4>), dim3((unsigned)tiles), dim3(256), bytes, stream, a);
-    else hipLaunchKernelGGL((fp8_tile_kernel<FA, FB, 2, 2>), dim3((unsigned)tiles), dim3(256), bytes, stream, a);
+    // pieces begin where a word of scale bytes does
+    a.chunk = ((a.k + p.pieces - 1) / p.pieces + 511) / 512 * 512;
+    const int pieces = (a.k + a.chunk - 1) / a.chunk;
+    a.ldp = p.ldp;
+    if (pieces == 1) a.partial = nullptr;
+    hipLaunchKernelGGL((fp8_tile_kernel<FA, FB, 2, 2>), dim3((unsigned)tiles_of(a.a.rows, a.b.rows, 128), (unsigned)pieces), dim3(256), (TileLds<2, 2>::BYTES), stream, a);
+    if (pieces > 1)
+        hipLaunchKernelGGL(fp8_join_kernel, dim3((unsigned)(((long long)a.a.rows * (a.ldp >> 2) + 255) / 256)), dim3(256), 0, stream, a, pieces);
     return hipGetLastError();
 }
 
-hipError_t launch_fp8_matmul(const Fp8Args& a, int fmt_a, int fmt_b, hipStream_t stream) {
-    if (a.a.rows > 64 && a.b.rows > 64) {
-        const long long wide = (long long)((a.a.rows + 255) / 256) * ((a.b.rows + 255) / 256);
-        const int shape = wide >= 256 ? 0 : 1;
-        if (fmt_a == FP8_E4M3 && fmt_b == FP8_E4M3) return launch_tiles<0, 0>(a, shape, stream);
-        if (fmt_a == FP8_E4M3) return launch_tiles<0, 1>(a, shape, stream);
-        if (fmt_b == FP8_E4M3) return launch_tiles<1, 0>(a, shape, stream);
-        return launch_tiles<1, 1>(a, shape, stream);
-    }
-    const dim3 grid((unsigned)((a.b.rows + 15) / 16), (unsigned)((a.a.rows + 63) / 64));
-    if (fmt_a == FP8_E4M3 && fmt_b == FP8_E4M3) hipLaunchKernelGGL((fp8_direct_kernel<0, 0, 4>), grid, dim3(256), 0, stream, a);
-    else if (fmt_a == FP8_E4M3) hipLaunchKernelGGL((fp8_direct_kernel<0, 1, 4>), grid, dim3(256), 0, stream, a);
-    else if (fmt_b == FP8_E4M3) hipLaunchKernelGGL((fp8_direct_kernel<1, 0, 4>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((fp8_direct_kernel<1, 1, 4>), grid, dim3(256), 0, stream, a);
-    return hipGetLastError();
+hipError_t launch_fp8_matmul(const Fp8Args& a, const Fp8Plan& p, int fmt_a, int fmt_b, hipStream_t stream) {
+    if (fmt_a == FP8_E4M3 && fmt_b == FP8_E4M3) return launch_kind<0, 0>(a, p, stream);
+    if (fmt_a == FP8_E4M3) return launch_kind<0, 1>(a, p, stream);
+    if (fmt_b == FP8_E4M3) return launch_kind<1, 0>(a, p, stream);
+    return launch_kind<1, 1>(a, p, stream);
 }
 
 }  // namespace tsr
