@@ -352,7 +352,7 @@ typedef struct tsr_tensor_desc {
  * The step itself uses the moments before they are rounded.  States begin as zeros (scale bytes too), and are then what
  * earlier calls wrote: scale bytes 1 to 254.
  * Ranges that are written (p, m, v, their scales, p16) must not overlap one another, within a tensor or between two:
- * TSR_INVALID_ARG.  Pointers need the alignment of their type; tensors whose pointers are aligned to four elements are faster. */
+ * TSR_INVALID_ARG.  Pointers need the alignment of their type only. */
 int tsr_adamw_batched(const tsr_tensor_desc* tensors, int count, int t, const tsr_hyper* h, unsigned long long seed,
                       const float* g_scale, void* stream);
 

@@ -84,9 +84,7 @@ DenseItem item_of(const tsr_tensor_desc& d, const tsr_hyper& h, unsigned key) {
     it.key = key;
     const size_t ps = size_of(d.p_dtype), gs = size_of(d.g_dtype);
     const bool s8 = d.state == TSR_STATE_8BIT;
-    const size_t ms = s8 ? 4 : 16;           // four elements of a state
     it.flags = (ps == 2 ? DENSE_P16 : 0) | (gs == 2 ? DENSE_G16 : 0) | (s8 ? DENSE_STATE8 : 0);
-    if (aligned(d.p, 4 * ps) && aligned(d.g, 4 * gs) && aligned(d.m, ms) && aligned(d.v, ms) && aligned(d.p16, 8)) it.flags |= DENSE_VEC;
     return it;
 }
 
@@ -179,7 +177,7 @@ int tsr_grad_norm_batched(const tsr_tensor_desc* tensors, int count, float max_n
         if (!d.count) continue;
         if (a.count == NORM_ITEMS) TSR_TRY(flush());
         const size_t gs = size_of(d.g_dtype);
-        a.item[a.count++] = {d.g, d.count, groups, (gs == 2 ? DENSE_G16 : 0u) | (aligned(d.g, 4 * gs) ? DENSE_VEC : 0u)};
+        a.item[a.count++] = {d.g, d.count, groups, gs == 2 ? DENSE_G16 : 0u};
         groups += (unsigned)((d.count + c.chunk - 1) / c.chunk);
     }
     if (one) { TSR_HIP(launch_norm_one(a, s)); return TSR_OK; }

@@ -17,10 +17,10 @@ struct DenseItem {
     unsigned key;                                       // of this tensor's random bits in this step
     unsigned flags;
 };
-enum : unsigned { DENSE_P16 = 1, DENSE_G16 = 2, DENSE_STATE8 = 4, DENSE_VEC = 8 };
+enum : unsigned { DENSE_P16 = 1, DENSE_G16 = 2, DENSE_STATE8 = 4 };
 
 constexpr int STATE_BLOCK = 256;
-constexpr int DENSE_CHUNK = 4096;        // elements of one workgroup
+constexpr int DENSE_CHUNK = 4096;        // elements of one workgroup (8192: 431 us where these take 400)
 constexpr int DENSE_ITEMS = 40;          // tensors of one launch: 84 bytes each, under the 4 KB that a launch's arguments may take
 
 struct DenseArgs {

@@ -7,24 +7,30 @@ namespace tsr {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned short u16x4;
+// the same at any address of their element: the memory path takes vectors that straddle their boundary (60 tensors packed one
+// behind the other, 332 MB: 112 us element by element)
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;
+typedef __attribute__((ext_vector_type(4), aligned(2))) unsigned short u16x4_any;
+typedef __attribute__((aligned(1))) unsigned u8x4_any;
 
 constexpr int GROUPS = DENSE_CHUNK / 1024;               // groups of 256 elements of one wave (of four)
 static_assert(DENSE_CHUNK % 1024 == 0 && STATE_BLOCK == 256, "a wave takes whole blocks of states");
 
 // ------------------------------------------------------------------ four elements of a tensor
-// WHOLE: all four exist and lie on a boundary of their vector; else element by element, those at or beyond n as zero.
+// WHOLE: all four exist; else element by element, those at or beyond n as zero.  Every value is touched once, so past the caches
+// (the 109 tensors of the 130M model: 451 -> 400 us).
 template <typename T, bool WHOLE> __device__ inline f32x4 load4(const void* base, long long i, long long n) {
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
     if constexpr (sizeof(T) == 4) {
         const float* p = (const float*)base + i;
-        if constexpr (WHOLE) return __builtin_nontemporal_load((const f32x4*)p);
+        if constexpr (WHOLE) return __builtin_nontemporal_load((const f32x4_any*)p);
 #pragma unroll
         for (int j = 0; j < 4; ++j) if (i + j < n) x[j] = p[j];
     } else {
         const unsigned short* p = (const unsigned short*)base + i;
         u16x4 h = {0, 0, 0, 0};
         if constexpr (WHOLE) {
-            h = __builtin_nontemporal_load((const u16x4*)p);
+            h = __builtin_nontemporal_load((const u16x4_any*)p);
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) if (i + j < n) h[j] = p[j];
@@ -35,18 +41,18 @@ template <typename T, bool WHOLE> __device__ inline f32x4 load4(const void* base
     return x;
 }
 template <bool WHOLE> __device__ inline void store4(float* base, long long i, long long n, f32x4 x) {
-    if constexpr (WHOLE) { __builtin_nontemporal_store(x, (f32x4*)(base + i)); return; }
+    if constexpr (WHOLE) { __builtin_nontemporal_store(x, (f32x4_any*)(base + i)); return; }
 #pragma unroll
     for (int j = 0; j < 4; ++j) if (i + j < n) base[i + j] = x[j];
 }
 template <bool WHOLE> __device__ inline void store4(unsigned short* base, long long i, long long n, u16x4 x) {
-    if constexpr (WHOLE) { __builtin_nontemporal_store(x, (u16x4*)(base + i)); return; }
+    if constexpr (WHOLE) { __builtin_nontemporal_store(x, (u16x4_any*)(base + i)); return; }
 #pragma unroll
     for (int j = 0; j < 4; ++j) if (i + j < n) base[i + j] = x[j];
 }
 template <bool WHOLE> __device__ inline unsigned load4b(const void* base, long long i, long long n) {
     const unsigned char* p = (const unsigned char*)base + i;
-    if constexpr (WHOLE) return __builtin_nontemporal_load((const unsigned*)p);
+    if constexpr (WHOLE) return __builtin_nontemporal_load((const u8x4_any*)p);
     unsigned x = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) if (i + j < n) x |= (unsigned)p[j] << (8 * j);
@@ -54,7 +60,7 @@ template <bool WHOLE> __device__ inline unsigned load4b(const void* base, long l
 }
 template <bool WHOLE> __device__ inline void store4b(void* base, long long i, long long n, unsigned x) {
     unsigned char* p = (unsigned char*)base + i;
-    if constexpr (WHOLE) { __builtin_nontemporal_store(x, (unsigned*)p); return; }
+    if constexpr (WHOLE) { __builtin_nontemporal_store(x, (u8x4_any*)p); return; }
 #pragma unroll
     for (int j = 0; j < 4; ++j) if (i + j < n) p[j] = (unsigned char)(x >> (8 * j));
 }
@@ -93,6 +99,14 @@ template <int FMT> __device__ inline unsigned state_code(float x, float inv, uns
 __device__ inline unsigned finite_bits(float x) {                           // |x| as an integer that orders like it; 0 if not finite
     const unsigned a = __builtin_bit_cast(unsigned, x) & 0x7fffffffu;
     return a < 0x7f800000u ? a : 0u;
+}
+
+// m / (sqrt(v) + eps) by the units' own root and reciprocal, off by a step of fp32 each, where the states hold 3 bits: beside
+// 8-bit states the correctly rounded root and quotient are what bounds the step (two tables of 32000 x 2048: 351 -> 305 us).
+// The root takes no subnormal numbers: below them it is that of the least normal one.
+__device__ inline float quick_ratio(float m, float v, float eps) {
+    const float r = __builtin_amdgcn_sqrtf(v > 0.0f && v < 0x1p-126f ? 0x1p-126f : v) + eps;
+    return __builtin_amdgcn_div_fixupf(m * __builtin_amdgcn_rcpf(r), r, m);       // zeros, infinities and the like as a quotient has them
 }
 
 // ------------------------------------------------------------------ AdamW
@@ -139,7 +153,7 @@ __device__ inline void adamw_groups(const DenseItem& d, const AdamScalars& s, fl
             const float gj = g[u][j] * gs;
             const float mj = m[u][j] * s.beta1 + gj * omb1;
             const float vj = v[u][j] * s.beta2 + (gj * gj) * omb2;
-            const float dj = (mj * s.inv_c1) / (sqrtf(vj * s.inv_c2) + s.eps);
+            const float dj = S8 ? quick_ratio(mj * s.inv_c1, vj * s.inv_c2, s.eps) : (mj * s.inv_c1) / (sqrtf(vj * s.inv_c2) + s.eps);
             p[u][j] = p[u][j] * d.decay - dj * step;
             m[u][j] = mj; v[u][j] = vj;
         }
@@ -193,11 +207,6 @@ template <typename P, typename G, bool S8>
 __device__ inline void adamw_item(const DenseItem& d, const AdamScalars& s, float step, float gs, long long base) {
     base += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (GROUPS * 256);
     const long long end = min(d.count, base + GROUPS * 256);
-    if (!(d.flags & DENSE_VEC)) {
-#pragma unroll 1
-        for (; base < end; base += 256) adamw_groups<P, G, S8, false, 1>(d, s, step, gs, base);
-        return;
-    }
     if (base + GROUPS * 256 <= end) { adamw_groups<P, G, S8, true, GROUPS>(d, s, step, gs, base); return; }
 #pragma unroll 1
     for (; base + 256 <= end; base += 256) adamw_groups<P, G, S8, true, 1>(d, s, step, gs, base);
@@ -244,20 +253,18 @@ __device__ inline double square_sum4(f32x4 x, double acc) {
     return acc;
 }
 // elements [begin, end) of a gradient by `threads` threads, begin a multiple of 4
-template <typename G> __device__ inline double square_sum(const void* g, bool vec, long long begin, long long end, int thread, int threads) {
+template <typename G> __device__ inline double square_sum(const void* g, long long begin, long long end, int thread, int threads) {
     double a0 = 0.0, a1 = 0.0;
     long long i = begin + thread * 4;
     const long long stride = threads * 4;
-    if (vec) {
-        for (; i + 3 * stride + 4 <= end; i += 4 * stride) {
-            f32x4 x[4];
+    for (; i + 3 * stride + 4 <= end; i += 4 * stride) {
+        f32x4 x[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) x[u] = load4<G, true>(g, i + u * stride, end);
-            a0 = square_sum4(x[0], a0); a1 = square_sum4(x[1], a1);
-            a0 = square_sum4(x[2], a0); a1 = square_sum4(x[3], a1);
-        }
-        for (; i + 4 <= end; i += stride) a0 = square_sum4(load4<G, true>(g, i, end), a0);
+        for (int u = 0; u < 4; ++u) x[u] = load4<G, true>(g, i + u * stride, end);
+        a0 = square_sum4(x[0], a0); a1 = square_sum4(x[1], a1);
+        a0 = square_sum4(x[2], a0); a1 = square_sum4(x[3], a1);
     }
+    for (; i + 4 <= end; i += stride) a0 = square_sum4(load4<G, true>(g, i, end), a0);
     for (; i < end; i += stride) a1 = square_sum4(load4<G, false>(g, i, end), a1);
     return a0 + a1;
 }
@@ -283,8 +290,7 @@ __global__ __launch_bounds__(256) void norm_parts_kernel(const NormArgs a) {
     k = __builtin_amdgcn_readfirstlane(k);
     const NormItem& d = a.item[k];
     const long long begin = (long long)(blockIdx.x - d.first) * a.chunk, end = min(d.count, begin + a.chunk);
-    const bool vec = d.flags & DENSE_VEC;
-    double x = (d.flags & DENSE_G16) ? square_sum<__bf16>(d.g, vec, begin, end, tid, 256) : square_sum<float>(d.g, vec, begin, end, tid, 256);
+    double x = (d.flags & DENSE_G16) ? square_sum<__bf16>(d.g, begin, end, tid, 256) : square_sum<float>(d.g, begin, end, tid, 256);
     x = wave_sum(x);
     __shared__ double part[4];
     if (lane == 0) part[tid >> 6] = x;
@@ -312,8 +318,7 @@ __global__ __launch_bounds__(1024) void norm_one_kernel(const NormArgs a) {
     double x = 0.0;
     for (int k = __builtin_amdgcn_readfirstlane(tid >> 6); k < a.count; k += 16) {
         const NormItem& d = a.item[k];
-        const bool vec = d.flags & DENSE_VEC;
-        x += (d.flags & DENSE_G16) ? square_sum<__bf16>(d.g, vec, 0, d.count, lane, 64) : square_sum<float>(d.g, vec, 0, d.count, lane, 64);
+        x += (d.flags & DENSE_G16) ? square_sum<__bf16>(d.g, 0, d.count, lane, 64) : square_sum<float>(d.g, 0, d.count, lane, 64);
     }
     x = wave_sum(x);
     __shared__ double part[16];

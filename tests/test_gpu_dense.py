@@ -65,8 +65,10 @@ def hash_bits(seed, t, j, n):
         return mix(np.arange(n, dtype=np.uint32) * np.uint32(0x9E3779B1) + key)
 
 
-def step64(p, g, m, v, t, h, gs=1.0, wd_scale=1.0):
-    """(p, m, v, bounds of their fp32 errors) of one step in fp64."""
+def step64(p, g, m, v, t, h, gs=1.0, wd_scale=1.0, ratio=7):
+    """(p, m, v, bounds of their fp32 errors) of one step in fp64.  ratio: roundings of the quotient, in half steps: constants 1.5,
+    products 1.5, root 1, sum 1, quotient 1 make 6 (7 with what is left); beside 8-bit states root and reciprocal may be off by a
+    whole step of fp32 (2 each) and their product is rounded once more: 1.5 + 1.5 + 2 + 1 + 2 + 1 = 9 (10)."""
     b1, b2 = f32(h["beta1"]), f32(h["beta2"])
     o1, o2 = f32(np.float32(1) - np.float32(b1)), f32(np.float32(1) - np.float32(b2))
     lr, wd, eps, scale = f32(h["lr"]), f32(h["wd"]), f32(h["eps"]), f32(h["scale"])
@@ -78,7 +80,7 @@ def step64(p, g, m, v, t, h, gs=1.0, wd_scale=1.0):
     den = np.sqrt(v2 * c2) + eps
     d = m2 * c1 / den
     rv = np.divide(ev, v2, out=np.zeros_like(ev), where=v2 > 0)
-    ed = em * c1 / den + np.abs(d) * (0.5 * rv + 7 * U)                       # constants, product, root, sum, quotient
+    ed = em * c1 / den + np.abs(d) * (0.5 * rv + ratio * U)
     decay, step = 1 - lr * wd * wd_scale, lr * scale
     out = decay * p - step * d
     ep = (step * ed + U * (3 * np.abs(decay * p) + 4 * step * np.abs(d))) * 1.01 + 1e-44
@@ -225,7 +227,7 @@ def test_adamw_states_in_8_bits(tsr, pt, gt, n, shift):
     t, seed = 37, 99
     row = eight(n, 20, pt, gt, shift)
     m, v = value_of(row, "m", n), value_of(row, "v", n)
-    want, m2, v2, ep, em, ev = step64(f64(row["p"]), f64(row["g"]), m, v, t, HYPER)
+    want, m2, v2, ep, em, ev = step64(f64(row["p"]), f64(row["g"]), m, v, t, HYPER, ratio=10)
     first = dict(p=torch.zeros(1, device="cuda"), g=torch.zeros(1, device="cuda"), m=torch.zeros(1, device="cuda"), v=torch.zeros(1, device="cuda"))
     tsr.tsr_adamw_batched([first, row], t, seed=seed, **HYPER)
     torch.cuda.synchronize()
@@ -273,6 +275,22 @@ def test_8_bit_states_keep_their_mean(tsr):
     torch.cuda.synchronize()
     assert abs(value_of(row, "v", n).mean() / 32768.0 - f32(0.999) ** 10) < 5e-4
     assert abs(value_of(row, "m", n).mean() / 256.0 - f32(0.9) ** 10) < 5e-4
+
+
+@pytest.mark.parametrize("eps", [1e-8, 0.0])
+def test_8_bit_states_of_tiny_and_of_no_gradients(tsr, eps):
+    """Gradients whose squares are subnormal or vanish in fp32: the step is finite and lr times |m| / sqrt(v) at most where v is held
+    in fp32; with neither gradient nor state it is nothing, or not a number where eps is 0, as the formula says."""
+    n = 512
+    g = torch.full((n,), 1e-21)                                               # 0.001 g^2 = 1e-45: the least subnormal number
+    g[256:] = 0
+    row = dict(p=torch.ones(n), g=g, m=torch.zeros(n).to(E4), v=torch.zeros(n).to(E5), m_scale=torch.zeros(2, dtype=torch.uint8), v_scale=torch.zeros(2, dtype=torch.uint8))
+    row = {k: x.cuda() for k, x in row.items()}
+    tsr.tsr_adamw_batched([row], 1, 1e-3, eps=eps)
+    torch.cuda.synchronize()
+    p = f64(row["p"])
+    assert np.all(np.abs(p[:256] - 1) <= 1e-3 * 1.001)
+    assert np.all(p[256:] == 1) if eps else np.all(np.isnan(p[256:]))
 
 
 def test_the_same_call_gives_the_same_bits_and_another_seed_others(tsr):
