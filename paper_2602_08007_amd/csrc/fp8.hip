@@ -52,26 +52,43 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
     const int row0 = tile_m * 128, col0 = tile_n * 128;
     const int r0 = row0 + (tid >> 4) * 8, c0 = col0 + (tid & 15) * 8;
     float x[8][8];
+    if (row0 + 128 <= a.m && col0 + 128 <= a.n) {            // all loads in flight before the first is looked at
+        const long long at = (long long)r0 * a.ldx + c0;
+        if constexpr (X16) {
+            u16x8_any h[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const bool row_in = r0 + i < a.m;
-        const long long at = (long long)(r0 + i) * a.ldx + c0;
-        if (row_in && c0 + 8 <= a.n) {
-            if constexpr (X16) {
-                const u16x8_any h = *(const u16x8_any*)((const unsigned short*)a.X + at);
+            for (int i = 0; i < 8; ++i) h[i] = *(const u16x8_any*)((const unsigned short*)a.X + at + i * a.ldx);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[i][j] = __builtin_bit_cast(float, (unsigned)h[j] << 16);
-            } else {
-                const f32x4_any lo = *(const f32x4_any*)((const float*)a.X + at), hi = *(const f32x4_any*)((const float*)a.X + at + 4);
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[i][j] = __builtin_bit_cast(float, (unsigned)h[i][j] << 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float* from = (const float*)a.X + at + i * a.ldx;
+                const f32x4_any lo = *(const f32x4_any*)from, hi = *(const f32x4_any*)(from + 4);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) { x[i][j] = lo[j]; x[i][4 + j] = hi[j]; }
             }
-        } else {
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool row_in = r0 + i < a.m;
+            const long long at = (long long)(r0 + i) * a.ldx + c0;
+            if (!X16 && row_in && c0 + 8 <= a.n) {
+                const f32x4_any lo = *(const f32x4_any*)((const float*)a.X + at), hi = *(const f32x4_any*)((const float*)a.X + at + 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { x[i][j] = lo[j]; x[i][4 + j] = hi[j]; }
+                continue;
+            }
+            u16x8_any h = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (X16 && row_in && c0 + 8 <= a.n) h = *(const u16x8_any*)((const unsigned short*)a.X + at);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                x[i][j] = 0.0f;
-                if (row_in && c0 + j < a.n)
-                    x[i][j] = X16 ? __builtin_bit_cast(float, (unsigned)((const unsigned short*)a.X)[at + j] << 16) : ((const float*)a.X)[at + j];
+                const bool alone = row_in && c0 + 8 > a.n && c0 + j < a.n;
+                if (X16) x[i][j] = __builtin_bit_cast(float, (unsigned)(alone ? ((const unsigned short*)a.X)[at + j] : h[j]) << 16);
+                else x[i][j] = alone ? ((const float*)a.X)[at + j] : 0.0f;
             }
         }
     }
