@@ -333,7 +333,7 @@ typedef struct tsr_tensor_desc {
     unsigned char* m_scale; /* TSR_STATE_8BIT: one byte for each TSR_STATE_BLOCK values            */
     unsigned char* v_scale;
     void* p16;              /* optional: bf16 copy of the updated parameters (p_dtype TSR_F32)     */
-    long long count;        /* 0: nothing is done for this tensor                                  */
+    long long count;        /* 0: nothing is done for this tensor; 2^35 at most                    */
     int p_dtype, g_dtype;   /* TSR_F32 or TSR_BF16                                                 */
     int state;              /* tsr_state of m and v                                                */
     float wd_scale;         /* multiplies wd: 0 for gains and biases                               */
@@ -351,13 +351,13 @@ typedef struct tsr_tensor_desc {
  * consecutive elements (and what is left of the last one) as in tsr_fp8_quantize; a positive v is never rounded to zero.
  * The step itself uses the moments before they are rounded.  States begin as zeros (scale bytes too), and are then what
  * earlier calls wrote: scale bytes 1 to 254.
- * Ranges that are written (p, m, v, their scales, p16) must not overlap one another, within a tensor or between two:
- * TSR_INVALID_ARG.  Pointers need the alignment of their type only. */
+ * Ranges that are written (p, m, v, their scales, p16) must not overlap one another or what is read (g, g_scale), within
+ * a tensor or between two; gradients may be shared.  Else TSR_INVALID_ARG.  Pointers need the alignment of their type only. */
 int tsr_adamw_batched(const tsr_tensor_desc* tensors, int count, int t, const tsr_hyper* h, unsigned long long seed,
                       const float* g_scale, void* stream);
 
-/* norm = sqrt(sum of g.g over all tensors), and coef = max_norm / norm if norm > max_norm, else 1 (not a number if the
- * norm is not finite): the factor that tsr_adamw_batched takes as g_scale.  One float each on the device; coef may be
+/* norm = sqrt(sum of g.g over all tensors), and coef = max_norm / norm if norm > max_norm, else 1 (not a number if a
+ * gradient is not finite): the factor that tsr_adamw_batched takes as g_scale.  One float each on the device; coef may be
  * NULL.  max_norm > 0 (infinity: never clips).  Only g, g_dtype and count of the tensors are read.  Summed in fp64 in a
  * fixed order.  Workspace: tsr_grad_norm_workspace_bytes (0 if the arguments are not valid). */
 size_t tsr_grad_norm_workspace_bytes(const tsr_tensor_desc* tensors, int count);
@@ -379,7 +379,8 @@ int tsr_grad_norm_batched(const tsr_tensor_desc* tensors, int count, float max_n
  * nearest value (ties to even), and what is not finite becomes what the type has for it (e4m3: not a number).
  * q_dtype TSR_E4M3 or TSR_E5M2.  Q and Qt 16-byte aligned with leading dimensions that are multiples of 16, scales
  * 4-byte aligned with leading dimensions that are multiples of 4, else TSR_INVALID_ARG; bytes beyond the columns are left as
- * they are.  X needs the alignment of its type only. */
+ * they are.  X needs the alignment of its type only; outputs must not overlap it or one another.  m and n up to 2^30, and
+ * fewer than 2^24 tiles of 128 x 128, else TSR_BAD_SHAPE. */
 int tsr_fp8_quantize(const void* X, int x_dtype, int m, int n, long long ldx, int block_rows, int q_dtype,
                      void* Q, long long ldq, unsigned char* S, long long lds,
                      void* Qt, long long ldqt, unsigned char* St, long long ldst, void* stream);
@@ -389,7 +390,8 @@ int tsr_fp8_quantize(const void* X, int x_dtype, int m, int n, long long ldx, in
  * lies 2^-13 below it, so C is off by half a step of bf16 and by 2^-10 sum |a b| at most (measured on random data: by
  * 2e-5 of the norm), which is why there is no fp32 C.
  * A and B aligned as above; the bytes from a row's k values to the next multiple of 16, and from its scales to the next
- * multiple of 4, may be read but do not count.  m and n as they are, k up to 2^22.  C needs the alignment of its type only
+ * multiple of 4, may be read but do not count.  k and the leading dimensions of A and B up to 2^22, m and n
+ * up to 2^30 (where the other is at most 32, up to 2^28 - 16), m n up to 2^40, else TSR_BAD_SHAPE.  C needs the alignment of its type only
  * and must not overlap A, B or their scales.
  * Workspace: tsr_fp8_matmul_workspace_bytes, 0 for most sizes; where a small result is cut along k, a smaller workspace
  * means fewer pieces, and NULL none. */

@@ -452,7 +452,7 @@ def _device_of(*tensors) -> torch.device:
             dev = t.device
         elif t.device != dev:
             raise ValueError("tensors on different devices: %s and %s" % (dev, t.device))
-    if dev.type != "cuda":
+    if dev is None or dev.type != "cuda":
         raise TypeError("expected GPU tensors")
     return dev
 
@@ -485,8 +485,10 @@ class TensorSet:
     def __init__(self, tensors: Sequence[dict]):
         self._keep = [dict(t) for t in tensors]
         self.count = len(self._keep)
+        if not self.count:
+            raise ValueError("no tensors")
         self.only_g = any("p" not in t for t in self._keep)
-        self.descs = (tsr_tensor_desc * max(self.count, 1))()
+        self.descs = (tsr_tensor_desc * self.count)()
         self.device = _device_of(*(x for t in self._keep for x in t.values() if isinstance(x, torch.Tensor)))
         for d, t in zip(self.descs, self._keep):
             g = t["g"]
@@ -578,7 +580,7 @@ def _fp8_place(q, s, rows, cols, block_rows, name):
     """(pointer, ld, scale pointer, ld) of an output of the quantiser, or four empty places."""
     if q is None:
         return None, 0, None, 0
-    if tuple(q.shape) != (rows, cols) or s.dtype != torch.uint8 or tuple(s.shape) != (-(-rows // block_rows), -(-cols // 128)):
+    if s is None or tuple(q.shape) != (rows, cols) or s.dtype != torch.uint8 or tuple(s.shape) != (-(-rows // block_rows), -(-cols // 128)):
         raise ValueError("%s must be %d x %d with a uint8 scale for each %d x 128 of it" % (name, rows, cols, block_rows))
     return _ptr(q), _rows_ld(q), _ptr(s), _rows_ld(s)
 

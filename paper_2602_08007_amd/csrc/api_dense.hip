@@ -42,8 +42,8 @@ int check_tensor(const tsr_tensor_desc& d) {
 
 struct Range { uintptr_t begin, end; };
 
-// The ranges that the call writes, and whether two of them meet.
-int check_ranges(const tsr_tensor_desc* t, int count) {
+// The ranges that the call writes: whether two of them meet, or one of them something that is read only.
+int check_ranges(const tsr_tensor_desc* t, int count, const float* g_scale) {
     std::unique_ptr<Range[]> r(new (std::nothrow) Range[6 * (size_t)count]);
     if (!r) return TSR_OUT_OF_HOST_MEMORY;
     size_t k = 0;
@@ -65,6 +65,15 @@ int check_ranges(const tsr_tensor_desc* t, int count) {
     std::sort(r.get(), r.get() + k, [](const Range& a, const Range& b) { return a.begin < b.begin; });
     for (size_t i = 1; i < k; ++i)
         if (r[i].begin < r[i - 1].end) return TSR_INVALID_ARG;
+    // of the written ranges, which lie apart, the last that begins before what is read ends reaches furthest
+    auto written = [&](const void* p, long long bytes) {
+        const Range x{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes};
+        const Range* at = std::lower_bound(r.get(), r.get() + k, x.end, [](const Range& a, uintptr_t end) { return a.begin < end; });
+        return at != r.get() && at[-1].end > x.begin;
+    };
+    for (int i = 0; i < count; ++i)
+        if (t[i].count && written(t[i].g, t[i].count * (long long)size_of(t[i].g_dtype))) return TSR_INVALID_ARG;
+    if (g_scale && written(g_scale, 4)) return TSR_INVALID_ARG;
     return TSR_OK;
 }
 
@@ -116,7 +125,7 @@ int tsr_adamw_batched(const tsr_tensor_desc* tensors, int count, int t, const ts
     TSR_TRY(adam_scalars(a.s, t, h->beta1, h->beta2, h->eps));
     if (!aligned(g_scale, 4)) return TSR_INVALID_ARG;
     for (int i = 0; i < count; ++i) TSR_TRY(check_tensor(tensors[i]));
-    TSR_TRY(check_ranges(tensors, count));
+    TSR_TRY(check_ranges(tensors, count, g_scale));
     a.step = (float)((double)h->lr * (double)h->scale);
     a.g_scale = g_scale;
     const unsigned key = mix32(mix32(mix32((unsigned)seed) ^ (unsigned)(seed >> 32)) ^ (unsigned)t);

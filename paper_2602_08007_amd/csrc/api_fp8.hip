@@ -9,6 +9,7 @@ using namespace tsr;
 namespace {
 
 constexpr int MOST_K = 1 << 22;              // 256 rows of it lie within 31-bit offsets
+constexpr int MOST_ROWS = 1 << 30;           // a row's number and what is added to it stay within an int
 constexpr long long MOST_GROUPS = 1 << 24;   // workgroups of a launch: times 256 threads, 2^32
 
 bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
@@ -45,7 +46,7 @@ extern "C" {
 int tsr_fp8_quantize(const void* X, int x_dtype, int m, int n, long long ldx, int block_rows, int q_dtype,
                      void* Q, long long ldq, unsigned char* S, long long lds,
                      void* Qt, long long ldqt, unsigned char* St, long long ldst, void* stream) {
-    if (m <= 0 || n <= 0 || ldx < n || (block_rows != 1 && block_rows != 128)) return TSR_BAD_SHAPE;
+    if (m <= 0 || n <= 0 || m > MOST_ROWS || n > MOST_ROWS || ldx < n || (block_rows != 1 && block_rows != 128)) return TSR_BAD_SHAPE;
     if ((x_dtype != TSR_F32 && x_dtype != TSR_BF16) || !is_fp8(q_dtype)) return TSR_BAD_DTYPE;
     if (!X || !aligned(X, x_dtype == TSR_F32 ? 4 : 2) || (!Q && !Qt)) return TSR_INVALID_ARG;
     if ((long long)blocks(m, 128) * blocks(n, 128) >= MOST_GROUPS) return TSR_BAD_SHAPE;
@@ -57,7 +58,7 @@ int tsr_fp8_quantize(const void* X, int x_dtype, int m, int n, long long ldx, in
 }
 
 size_t tsr_fp8_matmul_workspace_bytes(int m, int n, int k) {
-    if (m <= 0 || n <= 0 || k <= 0 || k > MOST_K) return 0;
+    if (m <= 0 || n <= 0 || k <= 0 || m > MOST_ROWS || n > MOST_ROWS || k > MOST_K) return 0;
     const Fp8Plan p = fp8_plan(m, n, k);
     return p.pieces > 1 ? align_up((size_t)p.pieces * m * p.ldp * sizeof(float)) : 0;
 }
@@ -69,7 +70,8 @@ int tsr_fp8_matmul(const tsr_fp8_matrix* A, const tsr_fp8_matrix* B, int m, int 
     TSR_TRY(check_operand(B, k));
     if (!C || !aligned(C, 2)) return TSR_INVALID_ARG;
     // 2^40 elements are beyond any card; a result of few rows or columns takes a workgroup for every 16 of the others
-    if ((long long)m * n > (1ll << 40) || ((m <= 32 || n <= 32) && (m >= 16 * MOST_GROUPS || n >= 16 * MOST_GROUPS))) return TSR_BAD_SHAPE;
+    if (m > MOST_ROWS || n > MOST_ROWS || (long long)m * n > (1ll << 40)) return TSR_BAD_SHAPE;
+    if ((m <= 32 || n <= 32) && (m > 16 * (MOST_GROUPS - 1) || n > 16 * (MOST_GROUPS - 1))) return TSR_BAD_SHAPE;
     Fp8Args a{};
     a.a = operand(A, m); a.b = operand(B, n);
     a.k = k; a.C = C; a.ldc = ldc;

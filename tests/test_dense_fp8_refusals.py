@@ -140,3 +140,33 @@ def test_tensors_on_the_cpu_are_refused(tsr):
         tsr.TensorSet([dict(p=x, g=x, m=x, v=x)])
     with pytest.raises(TypeError):
         tsr.tsr_fp8_quantize(torch.zeros(4, 4), *tsr.fp8_matrix(4, 4, device="cpu"))
+
+
+def test_what_a_step_reads_is_not_what_it_writes(tsr):
+    d = tensors(tsr, 3)
+    own, other = FAKE + 0x200000, FAKE
+    # the gradient: its own p (in place, or by one element at either end), another tensor's states
+    for g in (own, own + 396, own - 396, own + 0x20000, other + 0x30000, other + 0x20000 + 396, other - 396):
+        assert adamw(tsr, tensors(tsr, 3, g=g)) == -1, hex(g)
+    assert adamw(tsr, tensors(tsr, 3, g=other + 0x40000, p16=other + 0x40000 + 396)) == -1
+    # the factor: within p, the last bytes of v
+    for at in (own, other + 0x30000 + 396, other + 0x20000 + 200):
+        assert adamw(tsr, d, g_scale=at) == -1, hex(at)
+
+
+@pytest.mark.parametrize("m,n", [((1 << 30) + 1, 64), ((1 << 31) - 1, 1), (64, (1 << 31) - 1), (1 << 28, 16), (16, (1 << 28) - 15), (1 << 21, 1 << 20)])
+def test_a_product_of_too_many_rows(tsr, m, n):
+    x = tsr.tsr_fp8_matrix(FAKE, FAKE, 208, 4, 2, 1)
+    assert tsr.lib.tsr_fp8_matmul(ctypes.byref(x), ctypes.byref(x), m, n, 200, FAKE, 1 << 31, None, 0, None) == -2
+
+
+@pytest.mark.parametrize("m,n", [((1 << 30) + 1, 1), (1, (1 << 31) - 1), (1 << 26, 1 << 12)])
+def test_a_quantised_matrix_of_too_many_rows(tsr, m, n):
+    assert tsr.lib.tsr_fp8_quantize(FAKE, 0, m, n, 1 << 31, 1, 2, FAKE, 1 << 31, FAKE, 1 << 24, None, 0, None, 0, None) == -2
+
+
+def test_no_tensors(tsr):
+    with pytest.raises(ValueError):
+        tsr.TensorSet([])
+    with pytest.raises(ValueError):
+        tsr.tsr_adamw_batched([], 1, 1e-3)

@@ -362,3 +362,16 @@ def test_norm_of_large_small_and_unfit_values(tsr):
         tsr.tsr_grad_norm_batched([dict(g=g)], float("inf"), norm, coef)
         torch.cuda.synchronize()
         assert coef.item() == 1.0
+
+
+def test_a_gradient_of_two_tensors(tsr):
+    """Tied gradients: read twice, each tensor steps as it does alone."""
+    g = si.normal((700,), si.stream_key(97, 1)).cuda()
+    p = [si.normal((700,), si.stream_key(97, 2 + i)).cuda() for i in range(2)]
+    alone = [x.clone() for x in p]
+    state = lambda: dict(m=torch.zeros(700, device="cuda"), v=torch.zeros(700, device="cuda"))      # noqa: E731
+    tsr.tsr_adamw_batched([dict(p=x, g=g, **state()) for x in p], 1, 1e-3)
+    for x in alone:
+        tsr.tsr_adamw_batched([dict(p=x, g=g, **state())], 1, 1e-3)
+    torch.cuda.synchronize()
+    assert torch.equal(p[0], alone[0]) and torch.equal(p[1], alone[1])

@@ -246,3 +246,25 @@ def test_matmul_gradients_of_a_linear_layer(tsr):
         # each factor of the unrounded product moved by half a step at most: 2^-4 (e4m3), 2^-3 (e5m2) of its value, below that
         # of the least octave of its block; as independent errors they add up to well under a tenth of the norm
         assert torch.linalg.norm(C - exact) / torch.linalg.norm(exact) < 0.1
+
+
+def test_matmul_with_less_workspace_than_it_would_take(tsr):
+    """A small result of a long contraction in fewer pieces, and in one without a workspace."""
+    m, n, k = 100, 200, 5000
+    ops = product_case(tsr, m, n, k, E4, E5, 1, 128, 902)
+    nbytes = tsr.tsr_fp8_matmul_workspace_bytes(m, n, k)
+    piece = m * n * 4
+    assert nbytes >= 3 * piece
+    for size in (nbytes, 3 * piece - 1, 2 * piece, piece, 1):
+        ws = tsr.workspace(nbytes)
+        ws.fill_(0xFF)
+        check_product(tsr, ops, m, n, k, 3, ws=ws[:size])
+        assert bool((ws[size:] == 0xFF).all())
+
+
+def test_quantize_without_a_place_for_the_scales(tsr):
+    x = torch.zeros(4, 4, device="cuda")
+    q, s = tsr.fp8_matrix(4, 4)
+    for places in ((q, None), (None, None, q, None), (None, s)):
+        with pytest.raises(ValueError):
+            tsr.tsr_fp8_quantize(x, *places)
