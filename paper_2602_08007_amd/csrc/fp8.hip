@@ -22,6 +22,8 @@ typedef __attribute__((ext_vector_type(4), aligned(2))) unsigned int u32x4_any;
 // wanted.  Blocks of one row: the largest of a row of the tile is found among the 16 threads of a row (moves within 16
 // lanes), that of a column among the threads of a column (two moves across the wave, then LDS).  The transposed tile goes
 // through LDS, whose rows are padded by 8 bytes.
+// Bound by memory: 16384 x 8192 bf16 both ways 120 us, 4.5 TB/s (a copy: 5.1), fp32 160 us, 5.0 TB/s; 16384 x 2048 bf16 31 us,
+// 4.3 TB/s.  All loads of a thread are in flight before the first is looked at.
 template <int FMT> __device__ inline unsigned fp8_encode4(const float* x) {        // nearest, |x| at most the largest value
     int w = 0;
     if constexpr (FMT == FP8_E4M3) {
@@ -225,7 +227,9 @@ __device__ inline i32x8 keep_bytes(i32x8 x, int valid) {
 }
 
 // Fragments straight from memory: 16 rows of B and 16 FM of A for a workgroup, whose four waves share the blocks of the
-// contraction among them and add up through LDS in a fixed order.
+// contraction among them and add up through LDS in a fixed order.  For few rows (or columns) of one operand: bound by reading the
+// other, which nobody shares.  1 x 5461 x 2048: 4.6 us, of which the 11 MB of B take 2.2 at the rate of a copy, the rest is the
+// launch and the first access; 32 rows: 8.8 us.
 template <int FA, int FB, int FM>
 __global__ __launch_bounds__(256) void fp8_direct_kernel(const Fp8Args g) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -301,17 +305,21 @@ __global__ __launch_bounds__(256) void fp8_direct_kernel(const Fp8Args g) {
 }
 
 // ------------------------------------------------------------------ product, tiles through LDS
-// A workgroup of four waves (2 x 2) computes 64 FM x 64 FN elements of C, each wave FM x FN tiles of 32 x 32, in blocks of 128
-// along the contraction (two instructions deep).  Rows of A and B go from memory straight into LDS, no registers between, 128
-// bytes of a row at a time: whole cache lines (in steps of 64 bytes every line came twice, its first half long gone when the
-// second was asked for: 2.15 against 2.9 PFLOP/s at 8192^3).  Two buffers: block p + 2 is asked for in the second step of
-// block p, when all fragments of p are in registers, and is needed in the second step of p + 1.
+// A workgroup of four waves (2 x 2) computes 128 x 128 elements of C, each wave 2 x 2 tiles of 32 x 32, in blocks of 128 along
+// the contraction (two instructions deep); two workgroups a compute unit.  Rows of A and B go from memory straight into LDS, no
+// registers between, 128 bytes of a row at a time: whole cache lines (in steps of 64 bytes every line came twice, its first half
+// long gone when the second was asked for).  Two buffers: block p + 2 is asked for in the second step of block p, when all
+// fragments of p are in registers, and is needed in the second step of p + 1.
 // LDS rows are 128 bytes, eight chunks of 16; chunk c of row r sits at c ^ ((r >> 1) & 7), which keeps the fragment reads (16
 // lanes at a time) free of bank conflicts.  The 32 rows of B of a tile are kept in the order in which the instruction hands its
 // results out, so that a lane ends up with 16 neighbouring elements of a row of C: row 8 j + 4 h + i of the instruction is row
 // 16 h + 4 j + i of B.
 // Scale bytes go through LDS too: for every block the word that holds its byte, again for each of its four blocks, so that
 // the loop is free of branches: the compiler moves matrix instructions across those.
+// Bound by the path from memory to LDS: a unit takes some 53 bytes a cycle there, and a tile of this size wants 32 KB for every
+// 512 cycles of its matrix instructions.  2736 x 1024 x 12345 in two pieces: 73 us, 0.95 PFLOP/s, and 6 for their sum (176 tiles
+// would leave 80 units idle); 2048 x 2048 x 2048: 14 us, 1.2 PFLOP/s.  Waves of 4 x 4 tiles of 16 x 16, which read a whole block's
+// fragments before they multiply, need fewer instructions but do not read beside the multiplication: 17 us.
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
@@ -331,21 +339,21 @@ __device__ inline void load_lds4(i32x4 rsrc, unsigned voff, unsigned to) {
 template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 #define TSR_PIN __builtin_amdgcn_sched_barrier(0)
 
-template <int FM, int FN> struct TileLds {
-    static constexpr int ROWS = 64 * (FM + FN), BUF = ROWS * 128;
+struct TileLds {
+    static constexpr int ROWS = 256, BUF = ROWS * 128;
     static constexpr int SCALES = 2 * BUF, BYTES = SCALES + 2 * ROWS * 4;
 };
 
 // With more than one piece (blockIdx.y) of the contraction each writes its fp32 sums, and fp8_join_kernel adds them up.
-template <int FA, int FB, int FM, int FN>
-__global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void fp8_tile_kernel(const Fp8Args whole_k) {
+template <int FA, int FB>
+__global__ __launch_bounds__(256, 2) void fp8_tile_kernel(const Fp8Args whole_k) {
     Fp8Args g = whole_k;
     const long long k_from = (long long)blockIdx.y * g.chunk;
     g.a.q += k_from; g.b.q += k_from;
     g.a.scale += k_from >> 7; g.b.scale += k_from >> 7;
     g.k = (int)min((long long)g.chunk, g.k - k_from);
-    using L = TileLds<FM, FN>;
-    constexpr int TM = 64 * FM, TN = 64 * FN, NF = FM + FN, NM = FM * FN;
+    using L = TileLds;
+    constexpr int FM = 2, FN = 2, TM = 64 * FM, TN = 64 * FN, NF = FM + FN, NM = FM * FN;
     constexpr unsigned OUT = 0x80000000u;                    // an offset beyond every operand: no access
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -536,7 +544,12 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void fp8_tile_kernel(co
 // LDS rows are 128 bytes (whole cache lines), eight chunks of 16; chunk c of row r sits at c ^ ((r >> 1) & 7): 16 lanes that
 // read the same chunk of 16 rows meet no bank twice.  The 64 rows of B of a wave are kept in the order in which the instruction
 // hands its results out: a lane ends up with 16 neighbouring elements of a row of C, 16 lanes apart with a whole line of it.
-// Scale bytes go through LDS as the words that hold them, one for every row and block, again for each of the word's four blocks.
+// Scale bytes go through LDS as the words that hold them, one for every row, once in four blocks: a wave keeps its words in
+// registers and shifts them on.
+// Bound by power: 8192 x 32000 x 2048 takes 497 us, 2.16 PFLOP/s; 8192^3 414 us, 2.65 PFLOP/s.  Of two kernels whose blocks take
+// 1100 and 1500 cycles the shorter ran at 1.7 GHz and the longer at 2.1, in the same time.  C costs 7 us a tile beside the 16
+// blocks of k = 2048.  Other forms, 8192^3: four waves of 128 x 128 each with their sums in the accumulation registers 440 us, with
+// loads spread over the block 437; four waves of 32 x 32 x 64 instructions 489.
 struct WideLds {
     static constexpr int BUF = 512 * 128, SCALES = 2 * BUF, BYTES = SCALES + 2 * 512 * 4;
 };
@@ -803,14 +816,14 @@ template <int FA, int FB> hipError_t launch_kind(Fp8Args a, const Fp8Plan& p, hi
         hipLaunchKernelGGL((fp8_wide_kernel<FA, FB>), dim3((unsigned)(tiles < 256 ? (tiles + 7) / 8 * 8 : 256)), dim3(512), WideLds::BYTES, stream, a);
         return hipGetLastError();
     }
-    const hipError_t e = allow_lds((const void*)fp8_tile_kernel<FA, FB, 2, 2>, TileLds<2, 2>::BYTES);
+    const hipError_t e = allow_lds((const void*)fp8_tile_kernel<FA, FB>, TileLds::BYTES);
     if (e != hipSuccess) return e;
     // pieces begin where a word of scale bytes does
     a.chunk = ((a.k + p.pieces - 1) / p.pieces + 511) / 512 * 512;
     const int pieces = (a.k + a.chunk - 1) / a.chunk;
     a.ldp = p.ldp;
     if (pieces == 1) a.partial = nullptr;
-    hipLaunchKernelGGL((fp8_tile_kernel<FA, FB, 2, 2>), dim3((unsigned)tiles_of(a.a.rows, a.b.rows, 128), (unsigned)pieces), dim3(256), (TileLds<2, 2>::BYTES), stream, a);
+    hipLaunchKernelGGL((fp8_tile_kernel<FA, FB>), dim3((unsigned)tiles_of(a.a.rows, a.b.rows, 128), (unsigned)pieces), dim3(256), TileLds::BYTES, stream, a);
     if (pieces > 1)
         hipLaunchKernelGGL(fp8_join_kernel, dim3((unsigned)(((long long)a.a.rows * (a.ldp >> 2) + 255) / 256)), dim3(256), 0, stream, a, pieces);
     return hipGetLastError();
