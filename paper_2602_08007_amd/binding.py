@@ -179,16 +179,15 @@ def workspace(nbytes: int, device="cuda") -> torch.Tensor:
 
 
 def _temp_workspace(nbytes: int, device, stream) -> torch.Tensor:
-    """Workspace for a one-shot call that did not bring its own.  It is dropped when the call
-    returns, while the kernels may still be queued: that is safe on torch's current stream (the
-    caching allocator reuses the block in stream order) and is made safe on any other stream by
-    telling the allocator which stream uses the block."""
-    ws = workspace(nbytes, device)
-    if stream is not None and isinstance(stream, torch.cuda.Stream) and stream != torch.cuda.current_stream(ws.device):
-        ws.record_stream(stream)
-    elif stream is not None and not isinstance(stream, torch.cuda.Stream):
+    """Workspace for a one-shot call that did not bring its own.  It is dropped when the call returns, while the kernels
+    may still be queued.  The caching allocator hands a block on in the order of the stream on which it was taken, so it is
+    taken on the one that uses it: a block of another stream's could still be in use by what is queued there."""
+    if stream is None:
+        return workspace(nbytes, device)
+    if not isinstance(stream, torch.cuda.Stream):
         raise ValueError("pass a torch.cuda.Stream, or an explicit ws together with a raw stream handle")
-    return ws
+    with torch.cuda.stream(stream):
+        return workspace(nbytes, device)
 
 
 def tsr_project_workspace_bytes(m: int, n: int, r: int) -> int:
