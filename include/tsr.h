@@ -349,8 +349,10 @@ typedef struct tsr_tensor_desc {
  * hash of (seed, t, place of the tensor in the array, index).  The same call on the same data gives the same bits.
  * 8-bit moments: value = 2^(byte - 127) times the 8-bit value, the byte chosen for each block of TSR_STATE_BLOCK
  * consecutive elements (and what is left of the last one) as in tsr_fp8_quantize; a positive v is never rounded to zero.
- * The step itself uses the moments before they are rounded.  States begin as zeros (scale bytes too), and are then what
- * earlier calls wrote: scale bytes 1 to 254.
+ * The step itself uses the moments before they are rounded.  Beside 8-bit moments its root and its quotient come from the
+ * units' approximations, each off by one step of fp32 at most (D: 10 half steps, 2^-24 of its value each, where the correctly
+ * rounded ones of 32-bit moments make 7).  States begin as zeros (scale bytes too), and are then what earlier calls wrote:
+ * scale bytes 1 to 254.
  * Ranges that are written (p, m, v, their scales, p16) must not overlap one another or what is read (g, g_scale), within
  * a tensor or between two; gradients may be shared.  Else TSR_INVALID_ARG.  Pointers need the alignment of their type only. */
 int tsr_adamw_batched(const tsr_tensor_desc* tensors, int count, int t, const tsr_hyper* h, unsigned long long seed,

@@ -103,9 +103,11 @@ __device__ inline unsigned finite_bits(float x) {                           // |
 
 // m / (sqrt(v) + eps) by the units' own root and reciprocal, off by a step of fp32 each, where the states hold 3 bits: beside
 // 8-bit states the correctly rounded root and quotient are what bounds the step (two tables of 32000 x 2048: 351 -> 305 us).
-// The root takes no subnormal numbers: below them it is that of the least normal one.
+// The root takes no subnormal numbers: those are multiplied by 2^24 before it and their root by 2^-12 after it, both exact.
 __device__ inline float quick_ratio(float m, float v, float eps) {
-    const float r = __builtin_amdgcn_sqrtf(v > 0.0f && v < 0x1p-126f ? 0x1p-126f : v) + eps;
+    const bool tiny = v < 0x1p-126f;
+    const float root = __builtin_amdgcn_sqrtf(v * (tiny ? 0x1p24f : 1.0f));
+    const float r = __builtin_fmaf(root, tiny ? 0x1p-12f : 1.0f, eps);
     return __builtin_amdgcn_div_fixupf(m * __builtin_amdgcn_rcpf(r), r, m);       // zeros, infinities and the like as a quotient has them
 }
 

@@ -375,3 +375,31 @@ def test_a_gradient_of_two_tensors(tsr):
         tsr.tsr_adamw_batched([dict(p=x, g=g, **state())], 1, 1e-3)
     torch.cuda.synchronize()
     assert torch.equal(p[0], alone[0]) and torch.equal(p[1], alone[1])
+
+
+@pytest.mark.parametrize("t", [1, 100000])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-20, 1e-8])
+def test_8_bit_states_whose_root_is_of_a_subnormal_number(tsr, t, eps):
+    """Second moments around and below the least normal fp32 number, where the unit's root takes no more values.  p is 0, so
+    that the step is what is seen.  Moments are computed as the kernel does, each product and sum rounded to fp32; from there on
+    root and reciprocal are off by a whole step of fp32 (2 half steps each), sum, product, and the product with lr by half a one:
+    7, and 1 for what is of second order and the rounding of lr."""
+    n = 2048
+    g = (10.0 ** (-23.0 + 6.0 * np.arange(n) / n)).astype(np.float32) * np.where(np.arange(n) % 3, 1, -1).astype(np.float32)
+    row = dict(p=torch.zeros(n), g=torch.from_numpy(g), m=torch.zeros(n).to(E4), v=torch.zeros(n).to(E5), m_scale=torch.zeros(n // 256, dtype=torch.uint8),
+               v_scale=torch.zeros(n // 256, dtype=torch.uint8))
+    row = {k: x.cuda() for k, x in row.items()}
+    tsr.tsr_adamw_batched([row], t, 1e-3, eps=eps)
+    torch.cuda.synchronize()
+    f = np.float32
+    b1, b2 = f(0.9), f(0.999)
+    m, v = g * (f(1) - b1), (g * g) * (f(1) - b2)
+    c1, c2 = f(1 / (1 - float(b1) ** t)), f(1 / (1 - float(b2) ** t))
+    m, v = m * c1, v * c2
+    assert (v == 0).sum() > 100 and ((v > 0) & (v < 2.0 ** -126)).sum() > 500 and (v >= 2.0 ** -126).sum() > 100
+    with np.errstate(divide="ignore"):
+        want = -f(1e-3).astype(np.float64) * (m.astype(np.float64) / (np.sqrt(v.astype(np.float64)) + float(f(eps))))
+    got = f64(row["p"])
+    big = np.isinf(want) | (np.abs(want) > 3.4e38)
+    assert np.array_equal(np.isinf(got), big) and np.array_equal(np.sign(got), np.sign(want))
+    assert np.all(np.abs(got[~big] - want[~big]) <= 8 * U * np.abs(want[~big]))
