@@ -351,8 +351,8 @@ typedef struct tsr_tensor_desc {
  * consecutive elements (and what is left of the last one) as in tsr_fp8_quantize; a positive v is never rounded to zero.
  * The step itself uses the moments before they are rounded.  Beside 8-bit moments its root and its quotient come from the
  * units' approximations, each off by one step of fp32 at most (D: 10 half steps, 2^-24 of its value each, where the correctly
- * rounded ones of 32-bit moments make 7).  States begin as zeros (scale bytes too), and are then what earlier calls wrote:
- * scale bytes 1 to 254.
+ * rounded ones of 32-bit moments make 7), and eps has to be 0 or between 2^-126 and 2^100, else TSR_INVALID_ARG.  States begin
+ * as zeros (scale bytes too), and are then what earlier calls wrote: scale bytes 1 to 254.
  * Ranges that are written (p, m, v, their scales, p16) must not overlap one another or what is read (g, g_scale), within
  * a tensor or between two; gradients may be shared.  Else TSR_INVALID_ARG.  Pointers need the alignment of their type only. */
 int tsr_adamw_batched(const tsr_tensor_desc* tensors, int count, int t, const tsr_hyper* h, unsigned long long seed,

@@ -124,7 +124,11 @@ int tsr_adamw_batched(const tsr_tensor_desc* tensors, int count, int t, const ts
     DenseArgs a{};
     TSR_TRY(adam_scalars(a.s, t, h->beta1, h->beta2, h->eps));
     if (!aligned(g_scale, 4)) return TSR_INVALID_ARG;
-    for (int i = 0; i < count; ++i) TSR_TRY(check_tensor(tensors[i]));
+    const bool eps8 = h->eps == 0.0f || (h->eps >= DENSE_EPS8_LEAST && h->eps <= DENSE_EPS8_MOST);
+    for (int i = 0; i < count; ++i) {
+        TSR_TRY(check_tensor(tensors[i]));
+        if (tensors[i].state == TSR_STATE_8BIT && !eps8) return TSR_INVALID_ARG;
+    }
     TSR_TRY(check_ranges(tensors, count, g_scale));
     a.step = (float)((double)h->lr * (double)h->scale);
     a.g_scale = g_scale;

@@ -20,6 +20,7 @@ struct DenseItem {
 enum : unsigned { DENSE_P16 = 1, DENSE_G16 = 2, DENSE_STATE8 = 4 };
 
 constexpr int STATE_BLOCK = 256;
+constexpr float DENSE_EPS8_LEAST = 0x1p-126f, DENSE_EPS8_MOST = 0x1p100f;     // of an eps beside 8-bit states that is not 0
 constexpr int DENSE_CHUNK = 4096;        // elements of one workgroup (8192: 431 us where these take 400)
 constexpr int DENSE_ITEMS = 40;          // tensors of one launch: 84 bytes each, under the 4 KB that a launch's arguments may take
 

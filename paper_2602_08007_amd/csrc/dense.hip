@@ -104,6 +104,8 @@ __device__ inline unsigned finite_bits(float x) {                           // |
 // m / (sqrt(v) + eps) by the units' own root and reciprocal, off by a step of fp32 each, where the states hold 3 bits: beside
 // 8-bit states the correctly rounded root and quotient are what bounds the step (two tables of 32000 x 2048: 351 -> 305 us).
 // The root takes no subnormal numbers: those are multiplied by 2^24 before it and their root by 2^-12 after it, both exact.
+// The reciprocal neither takes nor gives them: r is at least 2^-75 or 0 without eps, and the caller sees to an eps of 0 or
+// between 2^-126 and DENSE_EPS8_MOST = 2^100.
 __device__ inline float quick_ratio(float m, float v, float eps) {
     const bool tiny = v < 0x1p-126f;
     const float root = __builtin_amdgcn_sqrtf(v * (tiny ? 0x1p24f : 1.0f));

@@ -170,3 +170,8 @@ def test_no_tensors(tsr):
         tsr.TensorSet([])
     with pytest.raises(ValueError):
         tsr.tsr_adamw_batched([], 1, 1e-3)
+
+
+@pytest.mark.parametrize("eps", [1e-45, 1e-39, 1.3e30, float("inf")])
+def test_an_eps_that_the_step_beside_8_bit_states_cannot_take(tsr, eps):
+    assert adamw(tsr, tensors(tsr, 2, state=1, m_scale=FAKE + 0x140000, v_scale=FAKE + 0x150000), eps=eps) == -1
