@@ -78,7 +78,7 @@ int tsr_fp8_matmul(const tsr_fp8_matrix* A, const tsr_fp8_matrix* B, int m, int 
     Fp8Plan p = fp8_plan(m, n, k);
     if (p.pieces > 1) {                      // as many pieces as the workspace holds
         const size_t piece = (size_t)m * p.ldp * sizeof(float), fit = ws ? ws_bytes / piece : 0;
-        if ((size_t)p.pieces > fit) p.pieces = fit < 2 ? 1 : (int)fit;
+        if ((size_t)p.pieces > fit) p = fp8_plan(m, n, k, fit < 1 ? 1 : (int)fit);
         if (p.pieces > 1 && (uintptr_t)ws % ALIGN) return TSR_INVALID_ARG;
         a.partial = (float*)ws;
     }

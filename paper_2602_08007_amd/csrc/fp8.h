@@ -24,14 +24,15 @@ struct Fp8Args {
     void* C; long long ldc;     // bf16
     // set by the launch
     float* partial; long long ldp;       // pieces of the contraction: fp32 sums of each, rows of ldp
-    int chunk;                           // of k in a piece, a multiple of 512
+    int chunk;                           // of k in a piece, a multiple of 512 where there are several
     int groups_n;                        // of 16 rows of B
 };
 
 // How a product is done, by its sizes alone.
 enum { FP8_DIRECT = 0, FP8_TILES = 1, FP8_WIDE = 2 };
-struct Fp8Plan { int kind, pieces; long long ldp; };
-Fp8Plan fp8_plan(int m, int n, int k);
+struct Fp8Plan { int kind, pieces, chunk; long long ldp; };      // pieces of chunk along k, the last of what is left
+constexpr int FP8_PIECES = 16;
+Fp8Plan fp8_plan(int m, int n, int k, int most = FP8_PIECES);    // with `most` pieces at most
 hipError_t launch_fp8_matmul(const Fp8Args& a, const Fp8Plan& p, int fmt_a, int fmt_b, hipStream_t stream);
 
 }  // namespace tsr

@@ -775,9 +775,29 @@ namespace {
 long long tiles_of(int m, int n, int t) { return ((m + t - 1ll) / t) * ((n + t - 1ll) / t); }
 }
 
-Fp8Plan fp8_plan(int m, int n, int k) {
+// Tiles of 128 x 128 with the contraction in `most` pieces at most, each a multiple of 512 along k (where a word of scale bytes
+// begins) but for the last; which number of them is best, and its time in us beside what every form costs.  As measured on 583
+// sizes drawn at random up to 16384 x 16384 and k up to 60000, each in all its numbers of pieces: 4.5 ns for every step along k
+// while the tiles have a unit each, 1.2 times that for more than 256 of them and in proportion from 420 on; several pieces cost a
+// second launch, 2 us, and their sums written and read at 4 TB/s.  The choice is on average 2.5 % slower than the best one, 1.32
+// times at worst.  512 x 512 x 8192: 31 us whole, 18 in eight pieces; 2736 x 1024 x 12345: 82 and 74 in two; 2048 x 2048 x 2048:
+// 13.5 and 35 in two.
+static double fp8_cut(Fp8Plan& p, int m, int n, int k, int most) {
+    const double tiles = (double)tiles_of(m, n, 128);
+    double least = 0.0;
+    for (int s = 1; s <= most && (s - 1) * 512 < k; ++s) {
+        const int chunk = s == 1 ? k : ((k + s - 1) / s + 511) / 512 * 512, pieces = (k + chunk - 1) / chunk;
+        const double groups = tiles * pieces, share = groups <= 256.0 ? 1.0 : groups <= 420.0 ? 1.2 : groups / 350.0;
+        const double us = chunk * 0.0045 * share + (pieces == 1 ? 0.0 : 2.0 + pieces * ((double)m * n * 8.0 / 4e6));
+        if (s == 1 || us < least) { least = us; p.pieces = pieces; p.chunk = chunk; }
+    }
+    return least;
+}
+
+Fp8Plan fp8_plan(int m, int n, int k, int most) {
     Fp8Plan p{};
     p.pieces = 1;
+    p.chunk = k;
     p.ldp = (n + 3) & ~3ll;
     // few rows or columns: bound by reading the other operand (32 x 5461 x 2048: 8.8 us, in tiles 10.4; 64 rows: 13.8 and 11.5)
     if (m <= 32 || n <= 32) { p.kind = FP8_DIRECT; return p; }
@@ -785,17 +805,7 @@ Fp8Plan fp8_plan(int m, int n, int k) {
     // 4096 x 2048, 128 tiles: 31 and 23 us)
     if (tiles_of(m, n, 256) >= 160) { p.kind = FP8_WIDE; return p; }
     p.kind = FP8_TILES;
-    // Pieces of the contraction, at least 512 each: what the time in us is, as measured from 512 x 512 x 8192 (31 us whole, 16.5 in
-    // four) over 768 x 768 x 16384 (80; 28 in six) and 2736 x 1024 x 12345 (78; 68 in two) to 2048 x 2048 x 2048 (14; 35 in two):
-    // 4.5 ns for every step along k while the tiles fit the card at once, and for pieces a second launch and their sums
-    // written and read at 3 TB/s.
-    const double tiles = (double)tiles_of(m, n, 128);
-    double least = 0.0;
-    for (int s = 1; s <= 16 && (s == 1 || k / s >= 512); ++s) {
-        const double busy = tiles * s / 300.0;
-        const double us = k * 0.0045 * (busy > 1.0 ? busy : 1.0) / s + (s == 1 ? 0.0 : 3.0 + s * (double)m * n * 8.0 / 3e6);
-        if (s == 1 || us < least) { least = us; p.pieces = s; }
-    }
+    fp8_cut(p, m, n, k, most);
     return p;
 }
 
@@ -818,14 +828,12 @@ template <int FA, int FB> hipError_t launch_kind(Fp8Args a, const Fp8Plan& p, hi
     }
     const hipError_t e = allow_lds((const void*)fp8_tile_kernel<FA, FB>, TileLds::BYTES);
     if (e != hipSuccess) return e;
-    // pieces begin where a word of scale bytes does
-    a.chunk = ((a.k + p.pieces - 1) / p.pieces + 511) / 512 * 512;
-    const int pieces = (a.k + a.chunk - 1) / a.chunk;
+    a.chunk = p.chunk;
     a.ldp = p.ldp;
-    if (pieces == 1) a.partial = nullptr;
-    hipLaunchKernelGGL((fp8_tile_kernel<FA, FB>), dim3((unsigned)tiles_of(a.a.rows, a.b.rows, 128), (unsigned)pieces), dim3(256), TileLds::BYTES, stream, a);
-    if (pieces > 1)
-        hipLaunchKernelGGL(fp8_join_kernel, dim3((unsigned)(((long long)a.a.rows * (a.ldp >> 2) + 255) / 256)), dim3(256), 0, stream, a, pieces);
+    if (p.pieces == 1) a.partial = nullptr;
+    hipLaunchKernelGGL((fp8_tile_kernel<FA, FB>), dim3((unsigned)tiles_of(a.a.rows, a.b.rows, 128), (unsigned)p.pieces), dim3(256), TileLds::BYTES, stream, a);
+    if (p.pieces > 1)
+        hipLaunchKernelGGL(fp8_join_kernel, dim3((unsigned)(((long long)a.a.rows * (a.ldp >> 2) + 255) / 256)), dim3(256), 0, stream, a, p.pieces);
     return hipGetLastError();
 }
 

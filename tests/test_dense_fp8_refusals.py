@@ -175,3 +175,13 @@ def test_no_tensors(tsr):
 @pytest.mark.parametrize("eps", [1e-45, 1e-39, 1.3e30, float("inf")])
 def test_an_eps_that_the_step_beside_8_bit_states_cannot_take(tsr, eps):
     assert adamw(tsr, tensors(tsr, 2, state=1, m_scale=FAKE + 0x140000, v_scale=FAKE + 0x150000), eps=eps) == -1
+
+
+@pytest.mark.parametrize("m,n,k", [(100, 200, 5000), (128, 128, 4100), (64, 64, 8193), (512, 512, 8192), (768, 768, 16384), (2736, 1024, 12345), (40, 4000, 1 << 20)])
+def test_the_workspace_of_a_product_is_that_of_the_pieces_that_run(tsr, m, n, k):
+    """Pieces begin at multiples of 512 along k, so not every number of them exists: one that does gives itself back."""
+    nbytes, piece = tsr.tsr_fp8_matmul_workspace_bytes(m, n, k), m * -(-n // 4) * 16
+    pieces = nbytes // piece
+    assert pieces > 1 and nbytes == -(-pieces * piece // 256) * 256
+    chunk = -(-(-(-k // pieces)) // 512) * 512
+    assert -(-k // chunk) == pieces
