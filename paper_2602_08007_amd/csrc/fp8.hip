@@ -773,6 +773,7 @@ __global__ __launch_bounds__(256) void fp8_join_kernel(const Fp8Args g, int piec
 
 namespace {
 long long tiles_of(int m, int n, int t) { return ((m + t - 1ll) / t) * ((n + t - 1ll) / t); }
+int direct_rows(int m) { return m <= 16 ? 16 : m <= 32 ? 32 : 64; }       // rows of A of a workgroup without tiles
 }
 
 // Tiles of 128 x 128 with the contraction in `most` pieces at most, each a multiple of 512 along k (where a word of scale bytes
@@ -799,8 +800,21 @@ Fp8Plan fp8_plan(int m, int n, int k, int most) {
     p.pieces = 1;
     p.chunk = k;
     p.ldp = (n + 3) & ~3ll;
-    // few rows or columns: bound by reading the other operand (32 x 5461 x 2048: 8.8 us, in tiles 10.4; 64 rows: 13.8 and 11.5)
-    if (m <= 32 || n <= 32) { p.kind = FP8_DIRECT; return p; }
+    // Few rows or columns: bound by reading the other operand, straight from memory (32 x 5461 x 2048: 8.8 us, in tiles 10.4; 64
+    // rows: 13.8 and 11.5), unless the contraction is so long that its pieces in tiles gain more than the 4 us that they take
+    // longer to begin and to join: a step along k takes 0.8 to 2.4 ns while the workgroups have a unit each, twice that at least
+    // beyond (16 x 16 x 131072: 166 us, in tiles 35; 32 x 5461 x 8192: 34 and 17; 1 x 2048 x 8192: 9.6 and 10.3).  On 255 sizes drawn
+    // at random the choice is 0.9 % slower than the better one on average, 1.43 times at worst.
+    if (m <= 32 || n <= 32) {
+        const int rows = direct_rows(m);
+        const double groups = (double)(((n + 15ll) / 16) * ((m + rows - 1) / rows));
+        const double us = k * (rows == 16 ? 0.0008 : rows == 32 ? 0.0011 : 0.0024) * (groups <= 256.0 ? 1.0 : groups <= 512.0 ? 2.0 : groups / 256.0);
+        Fp8Plan tiles = p;
+        tiles.kind = FP8_TILES;
+        if (us > 4.0 + fp8_cut(tiles, m, n, k, most)) return tiles;
+        p.kind = FP8_DIRECT;
+        return p;
+    }
     // 160 tiles of 256 x 256 keep enough compute units busy (2048 x 5461 x 16384, 176 tiles: 224 us, in 128 x 128 241 us; 2048 x
     // 4096 x 2048, 128 tiles: 31 and 23 us)
     if (tiles_of(m, n, 256) >= 160) { p.kind = FP8_WIDE; return p; }
@@ -811,7 +825,7 @@ Fp8Plan fp8_plan(int m, int n, int k, int most) {
 
 template <int FA, int FB> hipError_t launch_kind(Fp8Args a, const Fp8Plan& p, hipStream_t stream) {
     if (p.kind == FP8_DIRECT) {
-        const int fm = a.a.rows <= 16 ? 1 : a.a.rows <= 32 ? 2 : 4;
+        const int fm = direct_rows(a.a.rows) / 16;
         a.groups_n = (int)((a.b.rows + 15ll) / 16);
         const dim3 grid((unsigned)((long long)a.groups_n * ((a.a.rows + 16 * fm - 1) / (16 * fm))));
         if (fm == 1) hipLaunchKernelGGL((fp8_direct_kernel<FA, FB, 1>), grid, dim3(256), 0, stream, a);

@@ -185,3 +185,8 @@ def test_the_workspace_of_a_product_is_that_of_the_pieces_that_run(tsr, m, n, k)
     assert pieces > 1 and nbytes == -(-pieces * piece // 256) * 256
     chunk = -(-(-(-k // pieces)) // 512) * 512
     assert -(-k // chunk) == pieces
+
+
+@pytest.mark.parametrize("m,n,k,cut", [(16, 16, 131072, True), (300, 7, 100000, True), (32, 5461, 8192, True), (1, 5461, 2048, False), (32, 5461, 2048, False), (3, 17, 129, False)])
+def test_a_long_contraction_of_few_rows_is_cut_into_pieces(tsr, m, n, k, cut):
+    assert (tsr.tsr_fp8_matmul_workspace_bytes(m, n, k) > 0) == cut

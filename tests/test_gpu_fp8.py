@@ -268,3 +268,12 @@ def test_quantize_without_a_place_for_the_scales(tsr):
     for places in ((q, None), (None, None, q, None), (None, s)):
         with pytest.raises(ValueError):
             tsr.tsr_fp8_quantize(x, *places)
+
+
+@pytest.mark.parametrize("m,n,k", [(16, 16, 70001), (5, 300, 20001), (300, 7, 20001), (1, 33, 40000), (32, 32, 5000)])
+def test_matmul_of_few_rows_and_a_long_contraction(tsr, m, n, k):
+    """With the workspace that it wants, with a third of it, and without."""
+    ops = product_case(tsr, m, n, k, E5, E4, 1, 128, 903)
+    nbytes = tsr.tsr_fp8_matmul_workspace_bytes(m, n, k)
+    for size in {nbytes, nbytes // 3, 1}:
+        check_product(tsr, ops, m, n, k, 2, ws=tsr.workspace(nbytes)[:size])
