@@ -277,3 +277,52 @@ def test_matmul_of_few_rows_and_a_long_contraction(tsr, m, n, k):
     nbytes = tsr.tsr_fp8_matmul_workspace_bytes(m, n, k)
     for size in {nbytes, nbytes // 3, 1}:
         check_product(tsr, ops, m, n, k, 2, ws=tsr.workspace(nbytes)[:size])
+
+
+def check_many_tiles(ops, C, m, n, k):
+    """C against fp64 on the GPU, in stripes of rows; the bound is check_product's."""
+    b = values(ops[2], ops[3], k).cuda().t().contiguous()
+    for r in range(0, m, 1024):
+        sa = ops[1][r:r + 1024] if ops[1].shape[0] == m else ops[1][r // 128:(r + 1024) // 128]
+        a = values(ops[0][r:r + 1024], sa, k).cuda()
+        want, got = a @ b, C[r:r + 1024].double()
+        bound = ((7 * 2.0 ** -13 + (k + 8) * 2.0 ** -23) * (a.abs() @ b.abs()) + 1e-40) * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs()
+        err = (got - want).abs()
+        assert bool((err <= bound).all()), (r, (err / bound).max().item())
+        assert torch.linalg.norm(got - want) <= (2.0 ** -8 + 2.0 ** -12) * torch.linalg.norm(want)
+
+
+def random_operand(tsr, rows, k, dt, block_rows, gen):
+    """An 8-bit matrix made on the GPU, its padding not a number."""
+    q, s, *_ = matrix(tsr, rows, k, dt, block_rows)
+    x = torch.randn(rows, k, generator=gen, device="cuda") * torch.exp(torch.randn(rows, 1, generator=gen, device="cuda"))
+    tsr.tsr_fp8_quantize(x, q, s, block_rows=block_rows)
+    return [q, s]
+
+
+# 17 x 10 tiles of 256 x 256, ragged at both ends, a contraction of a dozen blocks that ends inside one
+@pytest.mark.parametrize("ta,tb", [(E4, E4), (E5, E4), (E4, E5), (E5, E5)])
+@pytest.mark.parametrize("ra,rb,pitch", [(1, 128, 8), (1, 1, 3), (128, 128, 0), (128, 1, 16)])
+def test_matmul_of_many_tiles_in_every_form(tsr, ta, tb, ra, rb, pitch):
+    m, n, k = 4200, 2504, 1500
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(31)
+    ops = random_operand(tsr, m, k, ta, ra, gen) + random_operand(tsr, n, k, tb, rb, gen)
+    buf = torch.full((m + 1, n + pitch), 3.0, device="cuda", dtype=torch.bfloat16)
+    tsr.tsr_fp8_matmul(*ops, buf[:m, :n])
+    torch.cuda.synchronize()
+    check_many_tiles(ops, buf[:m, :n], m, n, k)
+    assert bool((buf[:, n:] == 3.0).all()) and bool((buf[m] == 3.0).all())
+
+
+@pytest.mark.parametrize("m,n,k,ta", [(8200, 16504, 200, E4), (16390, 8200, 130, E5)])
+def test_matmul_of_a_result_that_the_caches_cannot_hold(tsr, m, n, k, ta):
+    """More than 2^27 results, which are written past the caches."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(32)
+    ops = random_operand(tsr, m, k, ta, 1, gen) + random_operand(tsr, n, k, E4, 128, gen)
+    buf = torch.full((m + 1, n + 8), 3.0, device="cuda", dtype=torch.bfloat16)
+    tsr.tsr_fp8_matmul(*ops, buf[:m, :n])
+    torch.cuda.synchronize()
+    check_many_tiles(ops, buf[:m, :n], m, n, k)
+    assert bool((buf[:, n:] == 3.0).all()) and bool((buf[m] == 3.0).all())
