@@ -816,8 +816,9 @@ Fp8Plan fp8_plan(int m, int n, int k, int most) {
         return p;
     }
     // 160 tiles of 256 x 256 keep enough compute units busy (2048 x 5461 x 16384, 176 tiles: 224 us, in 128 x 128 241 us; 2048 x
-    // 4096 x 2048, 128 tiles: 31 and 23 us)
-    if (tiles_of(m, n, 256) >= 160) { p.kind = FP8_WIDE; return p; }
+    // 4096 x 2048, 128 tiles: 31 and 23 us), unless half of every tile or more is empty (64 x 41000 x 2048: 27 us, in 128 x 128 18;
+    // 128 x 65536 x 2048: 33 and 26; 129 x 65536 x 2048: 33 and 38)
+    if (m > 128 && n > 128 && tiles_of(m, n, 256) >= 160) { p.kind = FP8_WIDE; return p; }
     p.kind = FP8_TILES;
     fp8_cut(p, m, n, k, most);
     return p;

@@ -326,3 +326,15 @@ def test_matmul_of_a_result_that_the_caches_cannot_hold(tsr, m, n, k, ta):
     torch.cuda.synchronize()
     check_many_tiles(ops, buf[:m, :n], m, n, k)
     assert bool((buf[:, n:] == 3.0).all()) and bool((buf[m] == 3.0).all())
+
+
+@pytest.mark.parametrize("m,n,k", [(64, 41000, 300), (128, 41001, 130), (41000, 33, 260)])
+def test_matmul_of_many_tiles_that_would_be_half_empty(tsr, m, n, k):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(33)
+    ops = random_operand(tsr, m, k, E5, 1, gen) + random_operand(tsr, n, k, E4, 128, gen)
+    buf = torch.full((m + 1, n + 4), 3.0, device="cuda", dtype=torch.bfloat16)
+    tsr.tsr_fp8_matmul(*ops, buf[:m, :n])
+    torch.cuda.synchronize()
+    check_many_tiles(ops, buf[:m, :n], m, n, k)
+    assert bool((buf[:, n:] == 3.0).all()) and bool((buf[m] == 3.0).all())
