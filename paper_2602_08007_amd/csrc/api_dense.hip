@@ -172,8 +172,11 @@ int tsr_grad_norm_batched(const tsr_tensor_desc* tensors, int count, float max_n
     NormArgs a{};
     a.chunk = c.chunk;
     a.max_norm = max_norm; a.norm = norm; a.coef = coef;
-    // A few small gradients: one workgroup reads them in about the time that a second launch takes.
-    const bool one = c.total <= NORM_ONE && count <= NORM_ITEMS;
+    // A few small gradients: one workgroup, unless its 16 waves take longer for their stretches than a second launch does (fp32, in
+    // one and in two launches: 1 x 32768 3.75 and 4.9 us, 17 x 512 3.25 and 4.7, 64 x 512 4.6 and 4.75, 120 x 273 8.0 and 5.0).
+    long long stretches = 0;
+    for (int i = 0; i < count && count <= NORM_ITEMS; ++i) stretches += (tensors[i].count + NORM_STRETCH - 1) / NORM_STRETCH;
+    const bool one = c.total <= NORM_ONE && count <= NORM_ITEMS && stretches <= NORM_STRETCHES;
     unsigned groups = 0;
     long long done = 0;
     auto flush = [&]() -> int {
@@ -191,8 +194,10 @@ int tsr_grad_norm_batched(const tsr_tensor_desc* tensors, int count, float max_n
         if (a.count == NORM_ITEMS) TSR_TRY(flush());
         const size_t gs = size_of(d.g_dtype);
         a.item[a.count++] = {d.g, d.count, groups, gs == 2 ? DENSE_G16 : 0u};
-        groups += (unsigned)((d.count + c.chunk - 1) / c.chunk);
+        const long long each = one ? NORM_STRETCH : c.chunk;
+        groups += (unsigned)((d.count + each - 1) / each);
     }
+    a.stretches = groups;
     if (one) { TSR_HIP(launch_norm_one(a, s)); return TSR_OK; }
     TSR_TRY(flush());
     TSR_HIP(launch_norm_total((const double*)ws, (int)c.parts, max_norm, norm, coef, s));

@@ -38,14 +38,17 @@ hipError_t launch_adamw(const DenseArgs& a, unsigned workgroups, hipStream_t str
 constexpr int NORM_ITEMS = 120;
 constexpr int NORM_PARTS = 4096;         // partial sums of a call, one more at most for each tensor
 constexpr int NORM_CHUNK = 8192;         // least elements of one workgroup, and what its chunks are multiples of
-constexpr long long NORM_ONE = 1 << 15;  // up to so many elements in all, one workgroup does the whole call
+constexpr long long NORM_ONE = 1 << 15;  // up to so many elements in all, one workgroup does the whole call,
+constexpr int NORM_STRETCH = 1024;       // its waves so many at a time
+constexpr int NORM_STRETCHES = 64;       // and in so many stretches at most
 
-struct NormItem { const void* g; long long count; unsigned first; unsigned flags; };
+struct NormItem { const void* g; long long count; unsigned first; unsigned flags; };     // first workgroup, or stretch
 struct NormArgs {
     double* partial;                     // of this launch's first workgroup
     long long chunk;
     float max_norm; float* norm; float* coef;        // the call in one workgroup only
     int count;
+    unsigned stretches;                  // in one workgroup only
     NormItem item[NORM_ITEMS];
 };
 hipError_t launch_norm_parts(const NormArgs& a, unsigned workgroups, hipStream_t stream);

@@ -319,13 +319,18 @@ __global__ __launch_bounds__(1024) void norm_total_kernel(const double* partial,
     }
 }
 
-// A few small gradients: one workgroup, its waves take the tensors in turn.
+// A few small gradients: one workgroup, whose waves take stretches of NORM_STRETCH elements in turn, all loads of a stretch in
+// flight at once: a wave reads no more than the others, however the elements are spread over the tensors.
 __global__ __launch_bounds__(1024) void norm_one_kernel(const NormArgs a) {
     const int tid = threadIdx.x, lane = tid & 63;
     double x = 0.0;
-    for (int k = __builtin_amdgcn_readfirstlane(tid >> 6); k < a.count; k += 16) {
+    static_assert(NORM_ITEMS <= 128, "two tensors a lane");
+    const unsigned first0 = lane < a.count ? a.item[lane].first : ~0u, first1 = lane + 64 < a.count ? a.item[lane + 64].first : ~0u;
+    for (unsigned s = __builtin_amdgcn_readfirstlane(tid >> 6); s < a.stretches; s += 16) {
+        const int k = __builtin_amdgcn_readfirstlane((int)(__popcll(__ballot(first0 <= s)) + __popcll(__ballot(first1 <= s))) - 1);
         const NormItem& d = a.item[k];
-        x += (d.flags & DENSE_G16) ? square_sum<__bf16>(d.g, 0, d.count, lane, 64) : square_sum<float>(d.g, 0, d.count, lane, 64);
+        const long long begin = (long long)(s - d.first) * NORM_STRETCH, end = min(d.count, begin + NORM_STRETCH);
+        x += (d.flags & DENSE_G16) ? square_sum<__bf16>(d.g, begin, end, lane, 64) : square_sum<float>(d.g, begin, end, lane, 64);
     }
     x = wave_sum(x);
     __shared__ double part[16];

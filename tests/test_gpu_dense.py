@@ -403,3 +403,20 @@ def test_8_bit_states_whose_root_is_of_a_subnormal_number(tsr, t, eps):
     big = np.isinf(want) | (np.abs(want) > 3.4e38)
     assert np.array_equal(np.isinf(got), big) and np.array_equal(np.sign(got), np.sign(want))
     assert np.all(np.abs(got[~big] - want[~big]) <= 8 * U * np.abs(want[~big]))
+
+
+@pytest.mark.parametrize("gt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("sizes,shift", [([32768], 0), ([32767], 1), ([1, 1023, 1024, 1025, 20000, 3], 1), ([0, 2049, 0, 5], 0), ([273] * 120, 3), ([300] * 119 + [0], 0), ([32769], 0)])
+def test_norm_of_a_few_tensors_of_any_sizes(tsr, gt, sizes, shift):
+    """Every element counts once: squares are whole numbers, so their sum is exact, and half a step of fp32 is left for the root
+    and for the factor each (fp64 roots and quotients are off by far less)."""
+    gs, total = [], 0
+    for j, n in enumerate(sizes):
+        x = (torch.arange(n) * 7 + j) % 13 - 6
+        total += int(x.square().sum())
+        gs.append(offset(x.to(gt), shift)[0])
+    norm, coef = torch.full((1,), -1.0, device="cuda"), torch.full((1,), -1.0, device="cuda")
+    tsr.tsr_grad_norm_batched([dict(g=g) for g in gs], 1.0, norm, coef)
+    torch.cuda.synchronize()
+    want = np.sqrt(float(total))
+    assert abs(norm.item() - want) <= U * want * 1.0001 and abs(coef.item() - 1 / want) <= U / want * 1.0001
