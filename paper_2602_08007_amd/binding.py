@@ -585,11 +585,12 @@ def _fp8_place(q, s, rows, cols, block_rows, name):
 
 
 def _rows_ld(t: torch.Tensor) -> int:
-    """Leading dimension; that of a single column or row may be anything in torch, and is made one that holds the row."""
+    """Leading dimension.  What torch says of a single row's pitch or a single column's stride may be anything and is not
+    looked at; the pitch of a single row is made one that holds it."""
     ld, one = t.stride()
     if one != 1 and t.size(1) > 1:
         raise TypeError("expected a row-major 2-D tensor (unit column stride)")
-    return ld if t.size(0) > 1 else max(ld, -(-t.size(1) // 16) * 16)
+    return ld if t.size(0) > 1 else -(-t.size(1) // 16) * 16
 
 
 def tsr_fp8_quantize(X, Q=None, S=None, Qt=None, St=None, block_rows=1, stream=None):
@@ -601,7 +602,7 @@ def tsr_fp8_quantize(X, Q=None, S=None, Qt=None, St=None, block_rows=1, stream=N
         raise ValueError("give Q, Qt or both, of one type")
     q, ldq, s, lds = _fp8_place(Q, S, m, n, block_rows, "Q")
     qt, ldqt, st, ldst = _fp8_place(Qt, St, n, m, block_rows, "Qt")
-    _launch(dev, stream, _quantize, _ptr(X), _gdtype(X), m, n, _ld(X), block_rows, _fp8(some), q, ldq, s, lds, qt, ldqt, st, ldst)
+    _launch(dev, stream, _quantize, _ptr(X), _gdtype(X), m, n, _rows_ld(X), block_rows, _fp8(some), q, ldq, s, lds, qt, ldqt, st, ldst)
 
 
 def _fp8_operand(q, s, rows, k, name) -> tsr_fp8_matrix:

@@ -190,3 +190,16 @@ def test_the_workspace_of_a_product_is_that_of_the_pieces_that_run(tsr, m, n, k)
 @pytest.mark.parametrize("m,n,k,cut", [(16, 16, 131072, True), (300, 7, 100000, True), (32, 5461, 8192, True), (1, 5461, 2048, False), (32, 5461, 2048, False), (3, 17, 129, False)])
 def test_a_long_contraction_of_few_rows_is_cut_into_pieces(tsr, m, n, k, cut):
     assert (tsr.tsr_fp8_matmul_workspace_bytes(m, n, k) > 0) == cut
+
+
+def test_the_pitch_of_one_row_and_the_column_stride_of_one_column_do_not_matter(tsr):
+    """Whatever torch says of them: a single row is taken with a pitch that holds it, a single column with its own."""
+    import torch
+    from paper_2602_08007_amd import binding
+    row = torch.empty(3, 1000)[1:2, :200]
+    for x, ld in ((row, 208), (torch.empty(200, 1).t(), 208), (torch.empty(200).as_strided((1, 200), (0, 1)), 208), (torch.empty(1, 7).t(), 1), (torch.empty(5, 6)[:, 2:3], 6),
+                  (torch.empty(5, 6)[:, :4], 6)):
+        assert binding._rows_ld(x) == ld, (x.shape, x.stride())
+    for x in (torch.empty(6, 5).t(), torch.empty(6, 10)[:, ::2], torch.empty(1, 10)[:, ::2]):
+        with pytest.raises(TypeError):
+            binding._rows_ld(x)

@@ -338,3 +338,29 @@ def test_matmul_of_many_tiles_that_would_be_half_empty(tsr, m, n, k):
     torch.cuda.synchronize()
     check_many_tiles(ops, buf[:m, :n], m, n, k)
     assert bool((buf[:, n:] == 3.0).all()) and bool((buf[m] == 3.0).all())
+
+
+def test_rows_and_columns_of_other_tensors(tsr):
+    """One row out of a matrix whose pitch is no multiple of 16, or of a transposed column; one column of a transposed row."""
+    k, n = 200, 40
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(34)
+    x = torch.randn(k, 1, generator=gen, device="cuda")
+    want, scale = quantize64(x.cpu().t(), 1, E4)
+    wide = torch.zeros(4, 1000, dtype=torch.uint8, device="cuda").view(E4)        # row 2 begins 16-byte aligned
+    scales = torch.zeros(5, 6, dtype=torch.uint8, device="cuda")
+    q, s = wide[2:3, :k], scales[2:3, :2]
+    tsr.tsr_fp8_quantize(x.t(), q, s)
+    b, sb = random_operand(tsr, n, k, E4, 1, gen)
+    C = torch.zeros(1, n, device="cuda", dtype=torch.bfloat16)
+    tsr.tsr_fp8_matmul(q, s, b, sb, C)
+    qt, st, *_ = matrix(tsr, 1, k, E4, 1)
+    column = torch.empty(1, k, device="cuda").copy_(x.t()).t()                      # 200 x 1 with strides 1 and 200
+    tsr.tsr_fp8_quantize(column, Qt=qt, St=st)
+    torch.cuda.synchronize()
+    assert same_values(q, want) and torch.equal(s.cpu(), scale) and same_values(qt, want) and torch.equal(st.cpu(), scale)
+    rest = wide.view(torch.uint8).clone()
+    rest[2, :k] = 0
+    assert not rest.any() and int(scales[2, :2].min()) > 0 and int(scales.sum()) == int(scales[2, :2].sum())
+    want = values(q, s, k) @ values(b, sb, k).t()
+    assert torch.linalg.norm(C.cpu().double() - want) <= (2.0 ** -8 + 2.0 ** -12) * torch.linalg.norm(want)       # as in check_product
