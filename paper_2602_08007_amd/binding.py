@@ -456,6 +456,13 @@ def _device_of(*tensors) -> torch.device:
     return first.device
 
 
+def _int(n: int) -> int:
+    """n for a C int, of which ctypes would take the low 32 bits without a word."""
+    if not -0x80000000 <= n <= 0x7fffffff:
+        raise OverflowError("%d does not fit 32 bits" % n)
+    return n
+
+
 def _launch(dev: torch.device, stream, fn, *args) -> None:
     """fn(*args, stream) with the tensors' device current; the stream is that device's current one unless given."""
     at = dev.index
@@ -538,7 +545,7 @@ def tsr_adamw_batched(tensors, t, lr, wd=0.0, beta1=0.9, beta2=0.999, eps=1e-8, 
     if g_scale is not None and g_scale.device != s.device:
         raise ValueError("g_scale must lie on the tensors' device")
     h = tsr_hyper(lr, wd, beta1, beta2, eps, scale)
-    _launch(s.device, stream, _adamw, s.descs, s.count, t, ctypes.byref(h), seed, _ptr(g_scale))
+    _launch(s.device, stream, _adamw, s.descs, s.count, _int(t), ctypes.byref(h), seed, _ptr(g_scale))
 
 
 def tsr_grad_norm_workspace_bytes(tensors) -> int:
@@ -602,7 +609,7 @@ def tsr_fp8_quantize(X, Q=None, S=None, Qt=None, St=None, block_rows=1, stream=N
         raise ValueError("give Q, Qt or both, of one type")
     q, ldq, s, lds = _fp8_place(Q, S, m, n, block_rows, "Q")
     qt, ldqt, st, ldst = _fp8_place(Qt, St, n, m, block_rows, "Qt")
-    _launch(dev, stream, _quantize, _ptr(X), _gdtype(X), m, n, _rows_ld(X), block_rows, _fp8(some), q, ldq, s, lds, qt, ldqt, st, ldst)
+    _launch(dev, stream, _quantize, _ptr(X), _gdtype(X), _int(m), _int(n), _rows_ld(X), block_rows, _fp8(some), q, ldq, s, lds, qt, ldqt, st, ldst)
 
 
 def _fp8_operand(q, s, rows, k, name) -> tsr_fp8_matrix:
@@ -616,7 +623,7 @@ def _fp8_operand(q, s, rows, k, name) -> tsr_fp8_matrix:
 
 
 def tsr_fp8_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
-    return int(_matmul_ws(m, n, k))
+    return int(_matmul_ws(_int(m), _int(n), _int(k)))
 
 
 def tsr_fp8_matmul(A, SA, B, SB, C, ws=None, stream=None):
@@ -632,6 +639,6 @@ def tsr_fp8_matmul(A, SA, B, SB, C, ws=None, stream=None):
         nbytes = tsr_fp8_matmul_workspace_bytes(m, n, k)
         ws = _temp_workspace(nbytes, dev, stream) if nbytes else None
     a, b = _fp8_operand(A, SA, m, k, "A"), _fp8_operand(B, SB, n, k, "B")
-    _launch(dev, stream, _matmul, ctypes.byref(a), ctypes.byref(b), m, n, k, _ptr(C), _rows_ld(C), _ptr(ws),
+    _launch(dev, stream, _matmul, ctypes.byref(a), ctypes.byref(b), _int(m), _int(n), _int(k), _ptr(C), _rows_ld(C), _ptr(ws),
             0 if ws is None else ws.numel())
     return C

@@ -203,3 +203,36 @@ def test_the_pitch_of_one_row_and_the_column_stride_of_one_column_do_not_matter(
     for x in (torch.empty(6, 5).t(), torch.empty(6, 10)[:, ::2], torch.empty(1, 10)[:, ::2]):
         with pytest.raises(TypeError):
             binding._rows_ld(x)
+
+
+def test_numbers_that_do_not_fit_an_int_are_not_cut_to_its_low_bits(tsr, monkeypatch):
+    """ctypes takes the low 32 bits of a larger number: 2^32 + 4 rows would be taken as 4.  Without a GPU: tensors without storage,
+    and a stand-in for the launch."""
+    import torch
+    from paper_2602_08007_amd import binding
+    device, calls = torch.device("cuda", 0), []
+    monkeypatch.setattr(binding, "_device_of", lambda *t: device)
+    monkeypatch.setattr(binding, "_launch", lambda dev, stream, fn, *args: calls.append(args))
+    monkeypatch.setattr(binding, "_ptr", lambda t: None if t is None else FAKE)
+    monkeypatch.setattr(binding, "_temp_workspace", lambda *a: torch.empty(0))
+    E4, big = torch.float8_e4m3fn, (1 << 32) + 4
+    def pair(rows, cols):
+        return tsr.fp8_matrix(rows, cols, E4, device="meta")
+    x = torch.empty(4, 4, device="meta")
+    tsr.tsr_fp8_quantize(x, *pair(4, 4))
+    tsr.tsr_fp8_matmul(*pair(4, 4), *pair(4, 4), torch.empty(4, 4, dtype=torch.bfloat16, device="meta"))
+    assert len(calls) == 2
+    with pytest.raises(OverflowError):
+        tsr.tsr_fp8_quantize(torch.empty(big, 4, device="meta"), *pair(big, 4))
+    with pytest.raises(OverflowError):
+        tsr.tsr_fp8_quantize(torch.empty(4, big, device="meta"), *pair(4, big))
+    for m, n, k in ((big, 4, 4), (4, big, 4), (4, 4, big)):
+        with pytest.raises(OverflowError):
+            tsr.tsr_fp8_matmul(*pair(m, k), *pair(n, k), torch.empty(m, n, dtype=torch.bfloat16, device="meta"))
+        with pytest.raises(OverflowError):
+            tsr.tsr_fp8_matmul_workspace_bytes(m, n, k)
+    p = torch.empty(8, device="meta")
+    tsr.tsr_adamw_batched([dict(p=p, g=p, m=p, v=p)], 1, 1e-3)
+    with pytest.raises(OverflowError):
+        tsr.tsr_adamw_batched([dict(p=p, g=p, m=p, v=p)], (1 << 32) + 1, 1e-3)
+    assert len(calls) == 3
