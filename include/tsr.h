@@ -343,7 +343,7 @@ typedef struct tsr_tensor_desc {
  *   g <- *g_scale g (g_scale: one float on the device, or NULL for 1)
  *   m <- beta1 m + (1-beta1) g ; v <- beta2 v + (1-beta2) g.g ;
  *   D = (m / (1-beta1^t)) / (sqrt(v / (1-beta2^t)) + eps) ; p <- p - lr (scale D + wd wd_scale p)
- * t >= 1.  If *g_scale is not finite the step is left out: nothing is written.
+ * t >= 1; lr, wd, lr scale and lr wd wd_scale finite.  If *g_scale is not finite the step is left out: nothing is written.
  * A bf16 p (one without an fp32 master) and 8-bit moments are rounded stochastically, since rounding to the nearest
  * value would swallow most steps: up with the probability of the distance to the value below, decided by 16 bits of a
  * hash of (seed, t, place of the tensor in the array, index).  The same call on the same data gives the same bits.

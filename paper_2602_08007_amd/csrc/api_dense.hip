@@ -83,13 +83,17 @@ unsigned mix32(unsigned h) {                 // as the kernel's
     return h ^ (h >> 16);
 }
 
+float decay_of(const tsr_tensor_desc& d, const tsr_hyper& h) {
+    return (float)(1.0 - (double)h.lr * (double)h.wd * (double)d.wd_scale);
+}
+
 DenseItem item_of(const tsr_tensor_desc& d, const tsr_hyper& h, unsigned key) {
     DenseItem it{};
     it.p = d.p; it.g = d.g; it.m = d.m; it.v = d.v;
     it.m_scale = d.m_scale; it.v_scale = d.v_scale;
     it.p16 = (unsigned short*)d.p16;
     it.count = d.count;
-    it.decay = (float)(1.0 - (double)h.lr * (double)h.wd * (double)d.wd_scale);
+    it.decay = decay_of(d, h);
     it.key = key;
     const size_t ps = size_of(d.p_dtype), gs = size_of(d.g_dtype);
     const bool s8 = d.state == TSR_STATE_8BIT;
@@ -123,14 +127,15 @@ int tsr_adamw_batched(const tsr_tensor_desc* tensors, int count, int t, const ts
     if (count <= 0) return TSR_BAD_SHAPE;
     DenseArgs a{};
     TSR_TRY(adam_scalars(a.s, t, h->beta1, h->beta2, h->eps));
-    if (!aligned(g_scale, 4)) return TSR_INVALID_ARG;
+    a.step = (float)((double)h->lr * (double)h->scale);
+    if (!aligned(g_scale, 4) || !std::isfinite(h->lr) || !std::isfinite(h->wd) || !std::isfinite(a.step)) return TSR_INVALID_ARG;
     const bool eps8 = h->eps == 0.0f || (h->eps >= DENSE_EPS8_LEAST && h->eps <= DENSE_EPS8_MOST);
     for (int i = 0; i < count; ++i) {
         TSR_TRY(check_tensor(tensors[i]));
         if (tensors[i].state == TSR_STATE_8BIT && !eps8) return TSR_INVALID_ARG;
+        if (!std::isfinite(decay_of(tensors[i], *h))) return TSR_INVALID_ARG;
     }
     TSR_TRY(check_ranges(tensors, count, g_scale));
-    a.step = (float)((double)h->lr * (double)h->scale);
     a.g_scale = g_scale;
     const unsigned key = mix32(mix32(mix32((unsigned)seed) ^ (unsigned)(seed >> 32)) ^ (unsigned)t);
     unsigned groups = 0;                     // of the launch that is being filled

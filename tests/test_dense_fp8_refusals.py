@@ -236,3 +236,11 @@ def test_numbers_that_do_not_fit_an_int_are_not_cut_to_its_low_bits(tsr, monkeyp
     with pytest.raises(OverflowError):
         tsr.tsr_adamw_batched([dict(p=p, g=p, m=p, v=p)], (1 << 32) + 1, 1e-3)
     assert len(calls) == 3
+
+
+@pytest.mark.parametrize("change", [dict(lr=float("nan")), dict(lr=float("inf")), dict(wd=float("nan")), dict(wd=-float("inf")), dict(scale=float("nan")),
+                                    dict(lr=1e30, scale=1e30), dict(lr=1e30, wd=1e30)])
+def test_a_step_whose_factors_are_not_finite(tsr, change):
+    h = dict(lr=1e-3, wd=0.1, beta1=0.9, beta2=0.999, eps=1e-8, scale=1.0) | change
+    d = tensors(tsr)
+    assert tsr.lib.tsr_adamw_batched(d, 1, 1, ctypes.byref(tsr.tsr_hyper(**h)), 0, None, None) == -1
