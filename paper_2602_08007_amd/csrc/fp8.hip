@@ -328,13 +328,13 @@ __device__ inline i32x4 lds_rsrc(const void* p, long long bytes) {
     return i32x4{(int)(unsigned)a, (int)((unsigned)(a >> 32) & 0xffffu), (int)(bytes > 0x7fffffffLL ? 0x7fffffffLL : bytes), 0x00020000};
 }
 // 16 (or 4) bytes a lane from `rsrc` + voff to LDS at `to` + 16 (or 4) times the lane.  Not known to the compiler's counting
-// of loads in flight: whoever reads the place waits by wait_loads and a barrier.  m0 is set where it is used, declared as
-// overwritten, and read one wait state later (s_nop).
+// of loads in flight: whoever reads the place waits by wait_loads and a barrier.  m0 is set where it is used, and nothing else in
+// this file lives there; it is read one wait state later (s_nop).
 __device__ inline void load_lds16(i32x4 rsrc, unsigned voff, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "memory");
 }
 __device__ inline void load_lds4(i32x4 rsrc, unsigned voff, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "memory");
 }
 template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 #define TSR_PIN __builtin_amdgcn_sched_barrier(0)
