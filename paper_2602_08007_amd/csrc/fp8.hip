@@ -328,8 +328,10 @@ __device__ inline i32x4 lds_rsrc(const void* p, long long bytes) {
     return i32x4{(int)(unsigned)a, (int)((unsigned)(a >> 32) & 0xffffu), (int)(bytes > 0x7fffffffLL ? 0x7fffffffLL : bytes), 0x00020000};
 }
 // 16 (or 4) bytes a lane from `rsrc` + voff to LDS at `to` + 16 (or 4) times the lane.  Not known to the compiler's counting
-// of loads in flight: whoever reads the place waits by wait_loads and a barrier.  m0 is set where it is used, and nothing else in
-// this file lives there; it is read one wait state later (s_nop).
+// of loads in flight: whoever reads the place waits by wait_loads and a barrier.  m0 is set where it is used and read one wait
+// state later (s_nop).  It is a reserved register, which the compiler lets nobody declare as overwritten; it keeps nothing there for
+// itself, but sets it before each instruction of its own that reads it, and this file has none (no index into registers, no message,
+// no load into LDS by a builtin).
 __device__ inline void load_lds16(i32x4 rsrc, unsigned voff, unsigned to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "memory");
 }
