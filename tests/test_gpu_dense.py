@@ -420,3 +420,34 @@ def test_norm_of_a_few_tensors_of_any_sizes(tsr, gt, sizes, shift):
     torch.cuda.synchronize()
     want = np.sqrt(float(total))
     assert abs(norm.item() - want) <= U * want * 1.0001 and abs(coef.item() - 1 / want) <= U / want * 1.0001
+
+
+def test_a_run_with_8_bit_states_beside_one_with_32(tsr):
+    """400 steps on the same gradients, g = size (1 + noise) of an element.  Rounding keeps the mean but for what 16 random bits
+    cannot tell: each step up to 2^-16 of a step of the type is lost, a quarter of v at most, in 400 steps 400 2^-18 = 0.15 %.
+    Scatter of v: a step moves a value that lies on the grid by 0.001 |g^2 - v|, so it is rounded away from it with the
+    probability of that over the grid's step, at most v / 4: the variance of one rounding is at most 0.001 (g^2 + v) v / 4, of
+    all that are remembered 0.0005 v^2 / (1 - 0.999^2) = v^2 / 4, the standard deviation of the mean of 2^16 ratios 0.5 / 256.
+    Scatter of m: each rounding (m / 8)^2 / 4 at most, those remembered 1 / (1 - 0.9^2) of it, a standard deviation of 0.15.
+    p moves along m / sqrt(v): a scatter of v with variance w <= 1/4 lengthens that by 3/8 w and terms of higher order on
+    average, 0 to 20 %."""
+    n, steps = 1 << 16, 400
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(41)
+    size = torch.exp2(torch.rand(n, generator=gen, device="cuda") * 2 - 1) * 1e-3
+    g = torch.zeros(n, device="cuda")
+    full = dict(p=torch.zeros(n, device="cuda"), g=g, m=torch.zeros(n, device="cuda"), v=torch.zeros(n, device="cuda"))
+    held = dict(p=torch.zeros(n, device="cuda"), g=g, m=torch.zeros(n).to(E4).cuda(), v=torch.zeros(n).to(E5).cuda(),
+                m_scale=torch.zeros(n // 256, dtype=torch.uint8, device="cuda"), v_scale=torch.zeros(n // 256, dtype=torch.uint8, device="cuda"))
+    sets = [tsr.TensorSet([full]), tsr.TensorSet([held])]
+    for t in range(1, steps + 1):
+        g.copy_(size * (1 + torch.randn(n, generator=gen, device="cuda")))
+        for s in sets:
+            tsr.tsr_adamw_batched(s, t, 1e-3, seed=17)
+    torch.cuda.synchronize()
+    m = (value_of(held, "m", n) - f64(full["m"])) / f64(size)
+    v = value_of(held, "v", n) / f64(full["v"])
+    assert abs(v.mean() - 1) <= 5 * 0.5 / 256 + 400 * 2.0 ** -18 and v.std() <= 0.5
+    assert abs(m.mean()) <= 5 * 0.3 / 256                                     # |m| is twice the size at most, nearly always
+    moved = f64(held["p"]).sum() / f64(full["p"]).sum()
+    assert 0.98 <= moved <= 1.2, moved
