@@ -542,7 +542,8 @@ __global__ __launch_bounds__(256, 2) void fp8_tile_kernel(const Fp8Args whole_k)
 //   phase 2 q + 1  group 0 multiplies block q,   group 1 reads block q
 // In phase 2 q block q + 1 is asked for (A by group 0, B by group 1) into the buffer that block q - 1 has left; it is needed two
 // phases later.  Blocks are counted across tiles: the first block of the next tile is on its way while the last one of this
-// tile is multiplied, and a group writes its part of C while the other multiplies.
+// tile is multiplied, and a group begins to write its part of C while the other multiplies (the wait for its next loads is one for
+// these stores too).
 // LDS rows are 128 bytes (whole cache lines), eight chunks of 16; chunk c of row r sits at c ^ ((r >> 1) & 7): 16 lanes that
 // read the same chunk of 16 rows meet no bank twice.  The 64 rows of B of a wave are kept in the order in which the instruction
 // hands its results out: a lane ends up with 16 neighbouring elements of a row of C, 16 lanes apart with a whole line of it.
@@ -783,7 +784,7 @@ int direct_rows(int m) { return m <= 16 ? 16 : m <= 32 ? 32 : 64; }       // row
 // sizes drawn at random up to 16384 x 16384 and k up to 60000, each in all its numbers of pieces: 4.5 ns for every step along k
 // while the tiles have a unit each, 1.2 times that for more than 256 of them and in proportion from 420 on; several pieces cost a
 // second launch, 2 us, and their sums written and read at 4 TB/s.  The choice is on average 2.5 % slower than the best one, 1.32
-// times at worst.  512 x 512 x 8192: 31 us whole, 18 in eight pieces; 2736 x 1024 x 12345: 82 and 74 in two; 2048 x 2048 x 2048:
+// times at worst (on 273 other sizes 3.0 %, 1.39 times).  512 x 512 x 8192: 31 us whole, 18 in eight pieces; 2736 x 1024 x 12345: 82 and 74 in two; 2048 x 2048 x 2048:
 // 13.5 and 35 in two.
 static double fp8_cut(Fp8Plan& p, int m, int n, int k, int most) {
     const double tiles = (double)tiles_of(m, n, 128);
@@ -806,7 +807,7 @@ Fp8Plan fp8_plan(int m, int n, int k, int most) {
     // rows: 13.8 and 11.5), unless the contraction is so long that its pieces in tiles gain more than the 4 us that they take
     // longer to begin and to join: a step along k takes 0.8 to 2.4 ns while the workgroups have a unit each, twice that at least
     // beyond (16 x 16 x 131072: 166 us, in tiles 35; 32 x 5461 x 8192: 34 and 17; 1 x 2048 x 8192: 9.6 and 10.3).  On 255 sizes drawn
-    // at random the choice is 0.9 % slower than the better one on average, 1.43 times at worst.
+    // at random the choice is 0.9 % slower than the better one on average, 1.43 times at worst (100 others: 0.6 %, 1.32 times).
     if (m <= 32 || n <= 32) {
         const int rows = direct_rows(m);
         const double groups = (double)(((n + 15ll) / 16) * ((m + rows - 1) / rows));
