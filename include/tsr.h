@@ -363,7 +363,8 @@ int tsr_adamw_batched(const tsr_tensor_desc* tensors, int count, int t, const ts
 /* norm = sqrt(sum of g.g over all tensors), and coef = max_norm / norm if norm > max_norm, else 1 (not a number if a
  * gradient is not finite): the factor that tsr_adamw_batched takes as g_scale.  One float each on the device; coef may be
  * NULL.  max_norm > 0 (infinity: never clips).  Only g, g_dtype and count of the tensors are read.  Summed in fp64 in a
- * fixed order.  Workspace: tsr_grad_norm_workspace_bytes (0 if the arguments are not valid). */
+ * fixed order.  Workspace: tsr_grad_norm_workspace_bytes (0 if the arguments are not valid); norm, coef and it must not overlap
+ * the gradients or one another. */
 size_t tsr_grad_norm_workspace_bytes(const tsr_tensor_desc* tensors, int count);
 int tsr_grad_norm_batched(const tsr_tensor_desc* tensors, int count, float max_norm, float* norm, float* coef,
                           void* ws, size_t ws_bytes, void* stream);
