@@ -784,8 +784,8 @@ int direct_rows(int m) { return m <= 16 ? 16 : m <= 32 ? 32 : 64; }       // row
 // sizes drawn at random up to 16384 x 16384 and k up to 60000, each in all its numbers of pieces: 4.5 ns for every step along k
 // while the tiles have a unit each, 1.2 times that for more than 256 of them and in proportion from 420 on; several pieces cost a
 // second launch, 2 us, and their sums written and read at 4 TB/s.  The choice is on average 2.5 % slower than the best one, 1.32
-// times at worst (on 273 other sizes 3.0 %, 1.39 times).  512 x 512 x 8192: 31 us whole, 18 in eight pieces; 2736 x 1024 x 12345: 82 and 74 in two; 2048 x 2048 x 2048:
-// 13.5 and 35 in two.
+// times at worst (on 273 other sizes 3.0 %, 1.39 times).  512 x 512 x 8192: 31 us whole, 18 in eight pieces; 2736 x 1024 x 12345:
+// 82 and 74 in two; 2048 x 2048 x 2048: 13.5 and 35 in two.
 static double fp8_cut(Fp8Plan& p, int m, int n, int k, int most) {
     const double tiles = (double)tiles_of(m, n, 128);
     double least = 0.0;
